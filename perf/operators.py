@@ -180,7 +180,7 @@ def prepare(case: dict, seed: int) -> dict:
         from paper_2410_23668_amd.device import PagedKvCache
         s["pool"] = PagedKvCache.from_tensors(s["k"], s["v"], s["k_scale"], s["v_scale"])
         if c["op"] == "attention":
-            s["workspace"] = s["pool"].workspace(c["batch"], c["heads"])
+            s["workspace"] = s["pool"].workspace(c["batch"])
     return s
 
 

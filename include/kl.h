@@ -71,6 +71,7 @@ typedef enum {
 #define KL_DEVERR_TOKEN    1   /* a token id outside [0, vocab)                              */
 #define KL_DEVERR_POSITION 2   /* a position outside [0, capacity) or >= max_seq             */
 #define KL_DEVERR_BARRIER  4   /* a grid barrier waited longer than its watchdog allows      */
+#define KL_DEVERR_PAGE     8   /* a page table entry outside [0, n_pages)                    */
 
 /* Model shape.  Supported: head_dim 64 or 128, n_heads a multiple of
  * n_kv_heads with n_heads / n_kv_heads one of 1, 2, 4, 8 (and 3 with
@@ -240,6 +241,123 @@ kl_status kl_decode_step_noalloc(kl_state *st, const int32_t *token_ids,
                                  const int32_t *positions, int32_t batch, const kl_kv_cache *kv,
                                  float *logits_out, float *hidden_out, void *stream,
                                  int32_t mode);
+
+/* ---------------------------------------------------------------- paged cache
+ *
+ * A KV cache in pages: sequences of any length share one pool, and an 8-bit
+ * pool holds twice the positions of a bf16 one and halves what the attention
+ * reads.  Three operators work on one layer of a pool: kl_paged_append writes
+ * rows (a decode step's or a prompt's, quantised as they are written),
+ * kl_paged_read reads rows back, kl_paged_attention attends one new token per
+ * sequence over its cached positions.  All are asynchronous on 'stream',
+ * allocate nothing, synchronise nothing and may be captured into a graph.
+ *
+ * Conditions only the device can see set bits of the caller's device error
+ * word (int32, 4-byte aligned; NULL: not reported), with an atomic or; it is
+ * never cleared by these calls. */
+typedef enum {
+    KL_DTYPE_BF16 = 0,
+    KL_DTYPE_FP16 = 1,
+    KL_DTYPE_FP32 = 2,
+    KL_DTYPE_E4M3 = 3    /* OCP 8-bit float (4 exponent, 3 mantissa bits, largest 448) */
+} kl_dtype;
+
+/* The pool.  Entry (layer, page, head, offset) of k and v is a row of
+ * head_dim values: dev [n_layers][n_pages][n_kv_heads][page_size][head_dim],
+ * 16-byte aligned.  dtype KL_DTYPE_BF16: the values.  KL_DTYPE_E4M3: codes,
+ * value = code * 2^(s - 127) with the row's byte s (1..254) in k_scale,
+ * v_scale: dev [n_layers][n_pages][n_kv_heads][page_size], 8-byte aligned
+ * (NULL with KL_DTYPE_BF16).  A power of two costs an 8-bit float no
+ * precision (the significand is scaled by nothing), every product with it is
+ * exact, and a value read back is exact in bf16.
+ * page_size: a power of two, 8..4096.  head_dim: 64 or 128.  device: the HIP
+ * device of the pool, current in every call. */
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    int32_t dtype;
+    int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+    int32_t device;
+} kl_paged_cache;
+
+/* Which pages hold a sequence: position p of sequence b is in page
+ * pages[b * stride + p / page_size] at offset p % page_size (dev int32,
+ * stride >= max_pages elements).  Only entries of positions in use are read.
+ * max_pages * page_size < 2^31. */
+typedef struct {
+    const int32_t *pages;
+    int32_t batch, max_pages, stride;
+} kl_page_table;
+
+/* Rows of heads: element i of head h of row r at data + r * row_stride +
+ * h * head_stride + i (strides in elements, >= 0; of outputs, where there is
+ * more than one row or head, >= head_dim).  dtype: KL_DTYPE_BF16, _FP16 or
+ * _FP32.  data is aligned to its element. */
+typedef struct {
+    void *data;
+    int32_t dtype;
+    int64_t row_stride, head_stride;
+} kl_rows;
+
+/* Writes rows 0..rows-1 of k and v (n_kv_heads heads each) to the slots of
+ * (seq[r], positions[r]); seq NULL: row r is sequence r's.
+ *   seq        dev int32 [rows] or NULL (then rows <= table->batch)
+ *   positions  dev int32 [rows]; a negative position: a padding row, skipped
+ * bf16 pool: values rounded to nearest even.  e4m3 pool, per row and head
+ * with a = max |x|: e = the smallest integer >= -126 with a <= 448 2^e, scale
+ * byte e + 127, code = x 2^-e rounded to nearest even; a row with an infinity
+ * or NaN reads back as NaN throughout.  Every other slot stays as it was.  Two
+ * rows with the same slot in one call leave it unspecified.
+ * Device error bits: KL_DEVERR_POSITION for a sequence outside [0, batch) or
+ * a position >= max_pages * page_size, KL_DEVERR_PAGE for a bad table entry;
+ * such a row is skipped. */
+kl_status kl_paged_append(const kl_paged_cache *cache, int32_t layer, const kl_page_table *table,
+                          const int32_t *seq, const int32_t *positions, int64_t rows,
+                          const kl_rows *k, const kl_rows *v, int32_t *error, void *stream);
+
+/* Reads the slots of (seq[r], positions[r]) into rows of k and v, rounded to
+ * their type (nearest even).  Arguments and error bits as for
+ * kl_paged_append; a padding row's output stays as it was, a bad row's is
+ * NaN.  With strides of a kl_kv_cache's layer and sequence as output, a
+ * sequence moves from pages to the contiguous cache of kl_decode_step. */
+kl_status kl_paged_read(const kl_paged_cache *cache, int32_t layer, const kl_page_table *table,
+                        const int32_t *seq, const int32_t *positions, int64_t rows,
+                        const kl_rows *k, const kl_rows *v, int32_t *error, void *stream);
+
+/* Bytes of the workspace of kl_paged_attention calls of up to 'batch'
+ * sequences (at most 4096) over this pool, with any number of heads (0 if an
+ * argument is invalid). */
+size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
+
+/* Attention of one new token per sequence (sequence b is row b of q and out)
+ * over its first lengths[b] cached positions, the new one's among them:
+ *   out_h = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q_h . k_j),
+ * j in [lengths[b] - window, lengths[b]) and >= 0 (window 0: from 0), query
+ * head h with KV head h / (n_heads / n_kv_heads).
+ *   lengths    dev int32 [batch]; 0: no position (a padded batch): the output
+ *              row is zero and its lse -infinity
+ *   q, out     n_heads heads; n_heads a multiple of n_kv_heads, at most 16
+ *              times as many
+ *   scale      finite
+ *   lse        dev fp32 [batch][n_heads] or NULL: max_j + ln sum_j of scale q.k
+ *              (what joins this result with one over other positions)
+ *   workspace  dev, 16-byte aligned, at least kl_paged_attention_workspace()
+ *              bytes, zeroed by the caller before its first use; every call
+ *              leaves it ready for the next one.  Calls that may run at the
+ *              same time (other streams, graphs replayed side by side) need a
+ *              workspace each.
+ * Scores, softmax and sums are held in 32 bits, and a sequence's result does
+ * not depend on timing (parts are joined in a fixed order).  Slots outside the
+ * attended positions do not affect the result, whatever they hold; a NaN or
+ * infinity in an attended slot makes the head's output non-finite.
+ * Device error bits: KL_DEVERR_POSITION for a length outside [0, max_pages *
+ * page_size], KL_DEVERR_PAGE for a bad table entry of an attended position;
+ * the sequence's output row and lse are then NaN. */
+kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
+                             const kl_page_table *table, const int32_t *lengths, const kl_rows *q,
+                             int32_t n_heads, float scale, int32_t window, const kl_rows *out,
+                             float *lse, void *workspace, size_t workspace_bytes, int32_t *error,
+                             void *stream);
 
 /* Bytes of ONE of the K or V buffers for the given batch and capacity
  * (0 if cfg is invalid). */

@@ -30,11 +30,19 @@ MODES = {"per_layer": KL_MODE_PER_LAYER, "looped": KL_MODE_LOOPED, "per_op": KL_
 KL_DEVERR_TOKEN = 1
 KL_DEVERR_POSITION = 2
 KL_DEVERR_BARRIER = 4
+KL_DEVERR_PAGE = 8
+
+KL_DTYPE_BF16 = 0
+KL_DTYPE_FP16 = 1
+KL_DTYPE_FP32 = 2
+KL_DTYPE_E4M3 = 3
 
 EXPORTED = ["kl_load_model", "kl_model_create", "kl_model_set_layer", "kl_model_set_globals",
             "kl_decode_step", "kl_decode_step_noalloc", "kl_decode_greedy", "kl_kv_cache_bytes",
             "kl_get_device_error",
-            "kl_get_info", "kl_set_trace", "kl_read_stream", "kl_free_model", "kl_last_error"]
+            "kl_get_info", "kl_set_trace", "kl_read_stream", "kl_free_model", "kl_last_error",
+            "kl_paged_append", "kl_paged_read", "kl_paged_attention",
+            "kl_paged_attention_workspace"]
 
 
 class kl_config(ctypes.Structure):
@@ -74,6 +82,24 @@ class kl_info(ctypes.Structure):
                 ("arena_bytes", ctypes.c_int64), ("scratch_bytes", ctypes.c_int64),
                 ("noalloc_scratch_bytes", ctypes.c_int64),
                 ("noalloc_scratch_limit", ctypes.c_int64)]
+
+
+class kl_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("device", ctypes.c_int32)]
+
+
+class kl_page_table(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("batch", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("stride", ctypes.c_int32)]
+
+
+class kl_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class KlError(RuntimeError):
@@ -122,6 +148,15 @@ def lib():
     L.kl_set_trace.restype = i32
     L.kl_read_stream.argtypes = [vp, ctypes.c_size_t, i32, vp, vp]
     L.kl_read_stream.restype = i32
+    pc, pt, pr = (ctypes.POINTER(t) for t in (kl_paged_cache, kl_page_table, kl_rows))
+    for fn in (L.kl_paged_append, L.kl_paged_read):
+        fn.argtypes = [pc, i32, pt, vp, vp, ctypes.c_int64, pr, pr, vp, vp]
+        fn.restype = i32
+    L.kl_paged_attention_workspace.argtypes = [pc, i32]
+    L.kl_paged_attention_workspace.restype = ctypes.c_size_t
+    L.kl_paged_attention.argtypes = [pc, i32, pt, vp, pr, i32, ctypes.c_float, i32, pr, vp, vp,
+                                     ctypes.c_size_t, vp, vp]
+    L.kl_paged_attention.restype = i32
     L.kl_free_model.argtypes = [vp]
     L.kl_free_model.restype = None
     L.kl_last_error.argtypes = []
@@ -226,6 +261,30 @@ def kl_set_trace(state: int, dev_buffer: int | None, max_phases: int) -> None:
 
 def kl_read_stream(buf: int, nbytes: int, workgroups: int, dev_out: int, stream: int) -> None:
     _check(lib().kl_read_stream(buf, nbytes, workgroups, dev_out, stream))
+
+
+def kl_paged_append(cache: kl_paged_cache, layer: int, table: kl_page_table, seq: int | None,
+                    positions: int, rows: int, k: kl_rows, v: kl_rows, error: int | None,
+                    stream: int) -> None:
+    _check(lib().kl_paged_append(cache, layer, table, seq, positions, rows, k, v, error, stream))
+
+
+def kl_paged_read(cache: kl_paged_cache, layer: int, table: kl_page_table, seq: int | None,
+                  positions: int, rows: int, k: kl_rows, v: kl_rows, error: int | None,
+                  stream: int) -> None:
+    _check(lib().kl_paged_read(cache, layer, table, seq, positions, rows, k, v, error, stream))
+
+
+def kl_paged_attention_workspace(cache: kl_paged_cache, batch: int) -> int:
+    return int(lib().kl_paged_attention_workspace(cache, batch))
+
+
+def kl_paged_attention(cache: kl_paged_cache, layer: int, table: kl_page_table, lengths: int,
+                       q: kl_rows, n_heads: int, scale: float, window: int, out: kl_rows,
+                       lse: int | None, workspace: int, workspace_bytes: int,
+                       error: int | None, stream: int) -> None:
+    _check(lib().kl_paged_attention(cache, layer, table, lengths, q, n_heads, scale, window, out,
+                                    lse, workspace, workspace_bytes, error, stream))
 
 
 def kl_free_model(state: int) -> None:

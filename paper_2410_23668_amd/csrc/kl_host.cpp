@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "kl.h"
+#include "kl_error.h"
 #include "kl_internal.h"
 
 using namespace kl;
@@ -52,7 +53,7 @@ struct kl_state {
     int own_max;                      // residual rows a workgroup owns, at most
 };
 
-namespace {
+namespace kl {
 
 thread_local std::string g_last_error;
 
@@ -66,13 +67,9 @@ kl_status fail(kl_status s, const char *fmt, ...) {
     return s;
 }
 
-#define HIP_TRY(expr)                                                                      \
-    do {                                                                                   \
-        hipError_t e_ = (expr);                                                            \
-        if (e_ != hipSuccess)                                                              \
-            return fail(e_ == hipErrorOutOfMemory ? KL_ERR_OUT_OF_MEMORY : KL_ERR_HIP,     \
-                        "%s failed: %s", #expr, hipGetErrorString(e_));                    \
-    } while (0)
+}  // namespace kl
+
+namespace {
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

@@ -1,0 +1,60 @@
+// The paged cache's kernels: their arguments and launchers (kl_paged.hip), for
+// the host entry points (kl_paged_host.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kl.h"
+
+namespace kl {
+
+constexpr int kMaxGroup = 16;        // query heads per KV head
+constexpr int kMaxPagedBatch = 4096; // sequences of an attention call
+
+// One layer of a pool.
+struct PagedLayer {
+    uint8_t *k, *v;                  // rows of values or codes
+    uint8_t *ks, *vs;                // scale bytes (e4m3)
+    int n_pages, nkv, page_log2, d;
+    bool e4m3;
+};
+
+struct PagedTable {
+    const int32_t *pages;
+    int batch, max_pages, stride;
+};
+
+// kl_paged_append and kl_paged_read
+struct RowParams {
+    PagedLayer c;
+    PagedTable t;
+    const int32_t *seq, *positions;
+    long long rows;
+    void *k, *v;                     // the caller's rows
+    int k_type, v_type;
+    long long k_row, k_head, v_row, v_head;   // strides, elements
+    bool k_vec, v_vec;               // 8 elements of a head may be moved as 16-byte words
+    int32_t *error;
+};
+hipError_t launch_paged_append(const RowParams &p, hipStream_t stream);
+hipError_t launch_paged_read(const RowParams &p, hipStream_t stream);
+
+// kl_paged_attention
+struct AttnParams {
+    PagedLayer c;
+    PagedTable t;
+    const int32_t *lengths;
+    const void *q;
+    void *out;
+    int q_type, out_type, nq, group;
+    long long q_row, q_head, out_row, out_head;
+    float scale;
+    int window;
+    float *lse;
+    int32_t *error;
+};
+hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream);
+
+}  // namespace kl

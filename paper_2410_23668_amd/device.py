@@ -8,6 +8,9 @@ import torch
 
 from . import binding as kb
 
+_DTYPES = {torch.bfloat16: kb.KL_DTYPE_BF16, torch.float16: kb.KL_DTYPE_FP16,
+           torch.float32: kb.KL_DTYPE_FP32, torch.float8_e4m3fn: kb.KL_DTYPE_E4M3}
+
 
 def _dev_u16(a, device) -> torch.Tensor:
     """Host bf16 bit patterns (uint16) -> device int16 tensor with the same bits
@@ -142,3 +145,129 @@ class KvCache:
 
     def host(self):
         return (self.k.cpu().numpy().view(np.uint16), self.v.cpu().numpy().view(np.uint16))
+
+
+class PagedKvCache:
+    """A pool of KV cache pages for sequences of any length: k and v
+    [L][pages][n_kv][page_size][d], bf16 or e4m3; an e4m3 pool has a scale byte
+    (biased exponent of a power of two) per row in k_scale and v_scale
+    [L][pages][n_kv][page_size].  Which pages hold a sequence is the caller's
+    to decide: a table [batch][max_pages] int32 of page numbers, of which only
+    those of positions in use are read."""
+
+    def __init__(self, model_cfg: dict, n_pages: int, page_size: int = 64,
+                 dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        shape = (model_cfg["n_layers"], n_pages, model_cfg["n_kv_heads"], page_size,
+                 model_cfg["head_dim"])
+        scales = [None, None]
+        if dtype == torch.float8_e4m3fn:
+            # (127: the codes of a cleared pool stand for themselves)
+            scales = [torch.full(shape[:-1], 127, dtype=torch.uint8, device=device)
+                      for _ in range(2)]
+        self._bind(torch.zeros(shape, dtype=dtype, device=device),
+                   torch.zeros(shape, dtype=dtype, device=device), *scales)
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+                     v_scale: torch.Tensor | None = None) -> "PagedKvCache":
+        """A pool over the caller's tensors (which stay in use)."""
+        self = cls.__new__(cls)
+        self._bind(k, v, k_scale, v_scale)
+        return self
+
+    def _bind(self, k, v, k_scale, v_scale):
+        assert k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype
+        assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn)
+        assert k.is_contiguous() and v.is_contiguous() and k.device == v.device
+        assert k.device.type == "cuda"
+        if k.dtype == torch.float8_e4m3fn:
+            for s in (k_scale, v_scale):
+                assert s is not None and s.dtype == torch.uint8 and s.shape == k.shape[:-1]
+                assert s.is_contiguous() and s.device == k.device
+        else:
+            assert k_scale is None and v_scale is None
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        L, pages, n_kv, ps, d = k.shape
+        self.n_kv, self.page_size, self.head_dim = n_kv, ps, d
+        self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.c = kb.kl_paged_cache(
+            k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+            None if v_scale is None else v_scale.data_ptr(), _DTYPES[k.dtype], L, pages, n_kv, ps, d,
+            self.device.index)
+
+    def _table(self, table: torch.Tensor) -> kb.kl_page_table:
+        assert table.dtype == torch.int32 and table.dim() == 2 and table.device == self.device
+        assert table.shape[1] <= 1 or table.stride(1) == 1
+        batch, n = table.shape
+        return kb.kl_page_table(table.data_ptr(), batch, n,
+                                table.stride(0) if batch > 1 else n)
+
+    def _rows(self, x: torch.Tensor, rows: int, heads: int) -> kb.kl_rows:
+        assert x.shape == (rows, heads, self.head_dim) and x.stride(2) == 1
+        assert x.device == self.device
+        return kb.kl_rows(x.data_ptr(), _DTYPES[x.dtype], x.stride(0), x.stride(1))
+
+    def _slots(self, positions, seq) -> tuple:
+        assert positions.dtype == torch.int32 and positions.dim() == 1
+        assert positions.is_contiguous() and positions.device == self.device
+        if seq is not None:
+            assert seq.dtype == torch.int32 and seq.shape == positions.shape
+            assert seq.is_contiguous() and seq.device == self.device
+        return seq.data_ptr() if seq is not None else None, positions.data_ptr(), positions.numel()
+
+    def append(self, layer: int, table: torch.Tensor, positions: torch.Tensor, k: torch.Tensor,
+               v: torch.Tensor, seq: torch.Tensor | None = None,
+               stream: torch.cuda.Stream | None = None) -> None:
+        """Rows [n][n_kv][d] of k and v to the slots of (seq[i], positions[i])
+        (seq None: row i is sequence i's; a negative position is skipped)."""
+        s, p, n = self._slots(positions, seq)
+        kb.kl_paged_append(self.c, layer, self._table(table), s, p, n,
+                           self._rows(k, n, self.n_kv), self._rows(v, n, self.n_kv),
+                           self.error.data_ptr(), stream_handle(stream))
+
+    def read(self, layer: int, table: torch.Tensor, positions: torch.Tensor, k: torch.Tensor,
+             v: torch.Tensor, seq: torch.Tensor | None = None,
+             stream: torch.cuda.Stream | None = None) -> None:
+        """The slots' values into rows [n][n_kv][d] of k and v (arguments as for append)."""
+        s, p, n = self._slots(positions, seq)
+        kb.kl_paged_read(self.c, layer, self._table(table), s, p, n,
+                         self._rows(k, n, self.n_kv), self._rows(v, n, self.n_kv),
+                         self.error.data_ptr(), stream_handle(stream))
+
+    def workspace(self, batch: int) -> torch.Tensor:
+        """A workspace for attention calls of up to 'batch' sequences, one after
+        the other (calls that may overlap, graphs replayed side by side
+        included, need one each)."""
+        n = kb.kl_paged_attention_workspace(self.c, batch)
+        if n == 0:
+            raise kb.KlError(kb.KL_ERR_INVALID_ARGUMENT, kb.kl_last_error())
+        return torch.zeros(n, dtype=torch.uint8, device=self.device)
+
+    def attention(self, layer: int, table: torch.Tensor, lengths: torch.Tensor, q: torch.Tensor,
+                  out: torch.Tensor, workspace: torch.Tensor, scale: float | None = None,
+                  window: int = 0, lse: torch.Tensor | None = None,
+                  stream: torch.cuda.Stream | None = None) -> None:
+        """One new token per sequence over its first lengths[b] positions: q and
+        out [batch][heads][d], lse [batch][heads] fp32; scale 1/sqrt(d) unless given."""
+        B, heads = q.shape[0], q.shape[1]
+        assert lengths.dtype == torch.int32 and lengths.shape == (B,) and lengths.is_contiguous()
+        assert lengths.device == self.device and table.shape[0] == B
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
+        assert workspace.device == self.device
+        if lse is not None:
+            assert lse.dtype == torch.float32 and lse.shape == (B, heads) and lse.is_contiguous()
+            assert lse.device == self.device
+        kb.kl_paged_attention(self.c, layer, self._table(table), lengths.data_ptr(),
+                              self._rows(q, B, heads), heads,
+                              self.head_dim ** -0.5 if scale is None else scale, window,
+                              self._rows(out, B, heads),
+                              lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
+                              workspace.numel(), self.error.data_ptr(), stream_handle(stream))
+
+    def device_error(self) -> int:
+        """Synchronizes; the error bits of this pool's calls so far, which are then cleared."""
+        code = int(self.error.item())
+        if code:
+            self.error.zero_()
+        return code

@@ -283,7 +283,7 @@ typedef struct {
 /* Which pages hold a sequence: position p of sequence b is in page
  * pages[b * stride + p / page_size] at offset p % page_size (dev int32,
  * stride >= max_pages elements).  Only entries of positions in use are read.
- * max_pages * page_size < 2^31. */
+ * max_pages * page_size <= 2^30. */
 typedef struct {
     const int32_t *pages;
     int32_t batch, max_pages, stride;

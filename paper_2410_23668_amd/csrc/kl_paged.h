@@ -12,6 +12,11 @@ namespace kl {
 
 constexpr int kMaxGroup = 16;        // query heads per KV head
 constexpr int kMaxPagedBatch = 4096; // sequences of an attention call
+constexpr int kPagedGroups = 256;    // workgroups of an attention call, at most
+// The workspace of an attention call: parts for any group and head_dim, then
+// the arrival counters (at the same place whatever the call's shape, so that a
+// workspace serves calls of all shapes).
+constexpr size_t kPagedPartBytes = (size_t)kPagedGroups * 2 * kMaxGroup * (128 + 2) * sizeof(float);
 
 // One layer of a pool.
 struct PagedLayer {
@@ -49,10 +54,13 @@ struct AttnParams {
     const void *q;
     void *out;
     int q_type, out_type, nq, group;
+    bool q_vec;                      // as k_vec
     long long q_row, q_head, out_row, out_head;
     float scale;
     int window;
     float *lse;
+    float *parts;                    // workspace: [workgroup][2][group][d + 2]
+    unsigned *arrived;               // workspace: [batch][nkv], zero between calls
     int32_t *error;
 };
 hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream);

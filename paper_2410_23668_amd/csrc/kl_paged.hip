@@ -2,8 +2,10 @@
 // to and read from pages, and the attention of one new token per sequence.
 
 #include <algorithm>
+#include <atomic>
 
 #include "kl_paged.h"
+#include "kl_paged_shares.h"
 #include "kl_step_impl.h"
 
 namespace kl {
@@ -213,6 +215,42 @@ hipError_t launch_paged_read(const RowParams &p, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------- attention
+//
+// Split-K flash decoding over pages.  A unit is a (sequence, KV head); its
+// attended positions are cut into tiles of 16 KiB of keys and values, and the
+// tiles of all units, one unit after the other, are dealt in equal contiguous
+// shares to the workgroups and within one to its eight waves, so that lengths
+// of any kind load every wave alike.  A wave goes through its tiles with a
+// running maximum and sum; a unit that lies inside its share it writes out,
+// of a unit cut by the share's ends it leaves its part (maximum, sum,
+// unnormalised output) in LDS.  The workgroup joins the parts there; what is
+// part of a unit of several workgroups goes to the workspace, and the last of
+// them to arrive (a counter per unit) joins all in workgroup order.
+//
+// All query heads of a KV head share one pass over its keys and values on the
+// matrix cores, in layouts that need no exchange between lanes:
+//   S^T = K Q^T  v_mfma_f32_16x16x32_bf16: A = 16 key rows, B = the queries as
+//                columns.  The rows of two such products, t = 0 and 1, are the
+//                positions 8 (r / 4) + 4 t + r % 4 of a block of 32, so that
+//                lane (k4, n) ends up with the scores of head n and positions
+//                8 k4 .. 8 k4 + 7: what the second product wants of it.
+//   O^T = V^T P^T  A = V^T: lane (k4, r) has loaded elements EV r .. EV r +
+//                EV - 1 (EV = d / 16) of the 8 positions, one load a position
+//                that covers the whole row; product m takes element m of each,
+//                pairs of positions put together by byte permutes.
+// e4m3 rows become bf16 (exactly) on the way, keys with their row's scale,
+// values without: theirs goes into the probabilities.  Queries of 32 or 16
+// bits that bf16 cannot hold, and the probabilities, are taken as several bf16
+// terms: three are all 24 bits of a float; two, 16 bits, where the output has
+// 16 bits (the weights are off by 2^-17, an eighth of its fp16 half-step at
+// most).  Softmax and sums are fp32; the maximum moves only when a score passes
+// it by 2^8, so the loop has no cross-lane step.
+
+constexpr int kAttnWaves = 8;
+constexpr int kAttnThreads = kAttnWaves * 64;
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float load1(const void *p, int type, long long i) {
     if (type == KL_DTYPE_FP32) return reinterpret_cast<const float *>(p)[i];
@@ -224,78 +262,579 @@ __device__ __forceinline__ void store1(void *p, int type, long long i, float x) 
     else reinterpret_cast<uint16_t *>(p)[i] = bits16(x, type);
 }
 
-// Element i of a pool's row.
-__device__ __forceinline__ float pool1(const PagedLayer &c, const uint8_t *p, const uint8_t *scale,
-                                       long long row, int D, int i) {
-    if (!c.e4m3) return bf2f(reinterpret_cast<const uint16_t *>(p)[row * D + i]);
-    return __builtin_amdgcn_cvt_f32_fp8(p[row * D + i], 0) * pow2_of(scale[row]);
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(unsigned, v);
+}
+// NT bf16 terms of 8 floats (x is left as what the terms do not hold)
+template <int NT>
+__device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+            if (i + 1 < NT) {
+                x[2 * j] -= bf_lo(w[j]);
+                x[2 * j + 1] -= bf_hi(w[j]);
+            }
+        }
+        t[i] = __builtin_bit_cast(bf16x8, w);
+    }
 }
 
-// One workgroup per (sequence, query head), its four waves every fourth
-// position each with a running maximum and sum, joined at the end.
-template <int D>
-__global__ void __launch_bounds__(256) kl_paged_attention_kernel(AttnParams p) {
-    constexpr int E = D / 64;
-    __shared__ float wm[4], wl[4], wo[4][D];
-    const int b = blockIdx.x / p.nq, h = blockIdx.x % p.nq, g = h / p.group;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int ps = 1 << p.c.page_log2;
-    int len = p.lengths[b];
-    bool bad = len < 0 || (long long)len > (long long)p.t.max_pages * ps;
-    if (bad) {
-        flag_error(p.error, KL_DEVERR_POSITION);
-        len = 0;
-    }
-    float q[E], o[E], m = -INFINITY, l = 0.f;
+template <int D, bool F8, bool Full>
+__global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(AttnParams p) {
+    constexpr int ES = F8 ? 1 : 2;
+    constexpr int NK = paged_tile(D, ES), NS = NK / 32;   // positions of a tile; blocks of 32
+    constexpr int RB = D * ES;                  // bytes of a row
+    constexpr int NC = RB / 64;                 // 16-byte loads of a key row per lane
+    constexpr int EV = D / 16, VW = EV * ES / 4;   // value elements, words per lane and position
+    constexpr int ST = D / 32;                  // steps of the first product
+    constexpr int QT = Full ? 3 : 1, PT = Full ? 3 : 2;   // terms of queries, probabilities
+    constexpr int WD = D + 2;                   // floats of a part of one head
+    constexpr int NE = 2 * kAttnWaves;          // parts in LDS
+
+    const int G = p.group, nkv = p.c.nkv, B = p.t.batch;
+    float *const part = reinterpret_cast<float *>(kl_smem);      // [NE][G][WD]
+    int *const unit = reinterpret_cast<int *>(part + NE * G * WD);   // [NE]: unit, -1: none
+    int *const ubeg = unit + NE, *const uend = ubeg + NE;        // its tiles
+    int *const wsum = uend + NE;                                 // [kAttnWaves + 1]
+    int *const last = wsum + kAttnWaves + 1;                     // [2]
+    int *const pre = last + 2;                                   // [B + 1] tiles of earlier sequences
+
+    const int tid = threadIdx.x, lane = tid & 63, k4 = lane >> 4, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int psl = p.c.page_log2, psm = (1 << psl) - 1;
+    const long long cap = (long long)p.t.max_pages << psl;
+
+    // a length's tiles; a length out of range counts as empty
+    auto length_of = [&](int b, bool &bad) {
+        const int len = p.lengths[b];
+        bad = len < 0 || (long long)len > cap;
+        return bad ? 0 : len;
+    };
+    if (tid < NE) unit[tid] = -1;
+    if (tid == 0) pre[0] = 0;
+    int base = 0;
+    for (int b0 = 0; b0 < B; b0 += kAttnThreads) {
+        const int b = b0 + tid;
+        bool bad;
+        int s = b < B ? paged_tiles(length_of(b, bad), p.window, NK) : 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        q[i] = load1(p.q, p.q_type, b * p.q_row + h * p.q_head + lane * E + i);
-        o[i] = 0.f;
-    }
-    for (int j = (p.window > 0 ? max(0, len - p.window) : 0) + wave; j < len; j += 4) {
-        const int page = p.t.pages[(long long)b * p.t.stride + (j >> p.c.page_log2)];
-        if (page < 0 || page >= p.c.n_pages) {
-            flag_error(p.error, KL_DEVERR_PAGE);
-            bad = true;
-            break;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = from_lane(s, max(lane - off, 0));
+            s += lane >= off ? o : 0;
         }
-        const long long row = (((long long)page * p.c.nkv + g) << p.c.page_log2) + (j & (ps - 1));
-        float s = 0.f;
+        if (lane == 63) wsum[wave] = s;
+        __syncthreads();
+        int add = base, all = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) s = fmaf(q[i], pool1(p.c, p.c.k, p.c.ks, row, D, lane * E + i), s);
-        s = wave_sum(s) * p.scale;
-        const float mn = fmaxf(m, s), a = __expf(m - mn), w = __expf(s - mn);
-        l = l * a + w;
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            o[i] = o[i] * a + w * pool1(p.c, p.c.v, p.c.vs, row, D, lane * E + i);
-        m = mn;
+        for (int w = 0; w < kAttnWaves; ++w) {
+            if (w < wave) add += wsum[w];
+            all += wsum[w];
+        }
+        if (b < B) pre[b + 1] = add + s;
+        base += all;
+        __syncthreads();
     }
-    if (bad) l = __builtin_nanf("");
-    wm[wave] = m;
-    wl[wave] = l;
+    const int T = __builtin_amdgcn_readfirstlane(base) * nkv;
+    // (a workgroup for every kAttnWaves tiles, so that each wave has one)
+    const int np = min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves);
+    const int wg = blockIdx.x;
+    if (wg >= np) return;
+    const int X0 = share_first(T, np, wg), X1 = share_first(T, np, wg + 1);
+    int x, x1;
+    split_range(X1 - X0, kAttnWaves, wave, x, x1);
+    x += X0;
+    x1 += X0;
+
+    // A place in the row of tiles.
+    struct At {
+        int b, g, t, nt;     // sequence, KV head, tile of the unit, its tiles
+        int len, start, t0;  // positions attended: [start, len); first tile
+        bool bad;
+    };
+    auto enter = [&](At &a, int b) {
+        a.b = b;
+        a.nt = __builtin_amdgcn_readfirstlane(pre[b + 1] - pre[b]);
+        a.len = __builtin_amdgcn_readfirstlane(length_of(b, a.bad));
+        a.start = paged_start(a.len, p.window);
+        a.t0 = paged_first_tile(a.len, p.window, NK);
+    };
+    auto find = [&](int i) {
+        int lo = 0, hi = B;   // pre[lo] nkv <= i < pre[hi] nkv
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__builtin_amdgcn_readfirstlane(pre[mid]) * nkv <= i) lo = mid;
+            else hi = mid;
+        }
+        At a;
+        enter(a, lo);
+        const int r = i - __builtin_amdgcn_readfirstlane(pre[lo]) * nkv;
+        a.g = r / a.nt;
+        a.t = r % a.nt;
+        return a;
+    };
+    auto next = [&](At a) {
+        if (++a.t == a.nt) {
+            a.t = 0;
+            if (++a.g == nkv) {
+                a.g = 0;
+                enter(a, a.b + 1);
+            }
+        }
+        return a;
+    };
+
+    // The pages of a tile, entry of the tile's i-th group of 8 positions in
+    // lane i (positions outside the attended ones: the nearest one's).
+    auto load_pages = [&](const At &a) {
+        if (a.len == 0) return 0;
+        const int pos = (a.t0 + a.t) * NK + 8 * (lane % (NK / 8));
+        return p.t.pages[(long long)a.b * p.t.stride +
+                         (min(max(pos, a.start), a.len - 1) >> psl)];
+    };
+    u32x4 kr[NS][2][NC];
+    unsigned vr[NS][8][VW];
+    u32x2 ksr[NS], vsr[NS];
+    bool page_bad = false;   // of the tile whose keys were asked for last
+    auto tile_inside = [&](const At &a) {
+        const int key0 = (a.t0 + a.t) * NK;
+        return key0 >= a.start && key0 + NK <= a.len;
+    };
+    // byte offset of the page's rows of head g, for the group of positions of
+    // lane 'from' of pages
+    auto page_row = [&](const At &a, int pages, int from) {
+        const int page = from_lane(pages, from);
+        return ((long long)page * nkv + a.g) << psl;
+    };
+    auto load_keys = [&](const At &a, int &pages) {
+        if (a.len == 0) return;
+        page_bad = __any((unsigned)pages >= (unsigned)p.c.n_pages);
+        if ((unsigned)pages >= (unsigned)p.c.n_pages) pages = 0;
+        const int key0 = (a.t0 + a.t) * NK;
+        const bool inside = tile_inside(a);
 #pragma unroll
-    for (int i = 0; i < E; ++i) wo[wave][lane * E + i] = o[i];
+        for (int s = 0; s < NS; ++s) {
+            const int gk = key0 + 32 * s + 8 * (n >> 2);
+            const long long r0 = page_row(a, pages, 4 * s + (n >> 2));
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                int key = gk + 4 * t + (n & 3);
+                if (!inside) key = min(max(key, a.start), a.len - 1);
+                const uint8_t *src = p.c.k + (r0 + (key & psm)) * RB + 16 * k4;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) kr[s][t][c] = ld_stream_16B(src + 64 * c);
+            }
+            if constexpr (F8) {
+                const int grp = inside ? gk : min(max(gk, a.start), a.len - 1) & ~7;
+                ksr[s] = *reinterpret_cast<const u32x2 *>(p.c.ks + r0 + (grp & psm));
+            }
+        }
+    };
+    auto load_values = [&](const At &a, int pages) {
+        if (a.len == 0) return;
+        const int key0 = (a.t0 + a.t) * NK;
+        const bool inside = tile_inside(a);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int gk = key0 + 32 * s + 8 * k4;
+            const long long r0 = page_row(a, pages, 4 * s + k4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                int key = gk + j;
+                if (!inside) key = min(max(key, a.start), a.len - 1);
+                const uint8_t *src = p.c.v + (r0 + (key & psm)) * RB + n * (EV * ES);
+                if constexpr (VW == 4) {
+                    const u32x4 w = ld_stream_16B(src);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vr[s][j][i] = w[i];
+                } else if constexpr (VW == 2) {
+                    const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(src));
+                    vr[s][j][0] = w[0];
+                    vr[s][j][1] = w[1];
+                } else {
+                    vr[s][j][0] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(src));
+                }
+            }
+            if constexpr (F8) {
+                const int grp = inside ? gk : min(max(gk, a.start), a.len - 1) & ~7;
+                vsr[s] = *reinterpret_cast<const u32x2 *>(p.c.vs + r0 + (grp & psm));
+            }
+        }
+    };
+
+    bf16x8 q[QT][ST];
+    auto load_q = [&](const At &a) {
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            const int d0 = F8 ? 64 * (s / 2) + 16 * k4 + 8 * (s & 1) : 32 * s + 8 * k4;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+            if (n < G) {
+                const long long at = a.b * p.q_row + (a.g * G + n) * p.q_head + d0;
+                load8(reinterpret_cast<const uint8_t *>(p.q) + at * (p.q_type == KL_DTYPE_FP32 ? 4 : 2),
+                      p.q_type, p.q_vec, v);
+            }
+            bf16x8 t[QT];
+            split_terms(v, t);
+#pragma unroll
+            for (int i = 0; i < QT; ++i) q[i][s] = t[i];
+        }
+    };
+
+    // output i = element dd of query head h of the group: O unnormalised, M
+    // the maximum (log2 units), L the sum
+    auto write_out = [&](int b, int g, int h, int dd, float O, float M, float L) {
+        store1(p.out, p.out_type, b * p.out_row + (g * G + h) * p.out_head + dd, O / L);
+        if (p.lse && dd == 0)
+            p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
+    };
+
+    if (x < x1) {
+        const float c = p.scale * 1.4426950408889634f;
+        const int first = x;
+        At a = find(x), an, ann;
+        int pg = load_pages(a), pgn = 0, pgnn = 0;
+        bool more = x + 1 < x1;
+        if (more) {
+            an = next(a);
+            pgn = load_pages(an);
+        }
+        load_keys(a, pg);
+        bool bad = a.bad || (a.len > 0 && page_bad);
+        load_values(a, pg);
+        load_q(a);
+        float m = -INFINITY, l = 0.f;
+        f32x4 o[EV];
+#pragma unroll
+        for (int i = 0; i < EV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (;;) {
+            const bool inside = tile_inside(a);
+            const int key0 = (a.t0 + a.t) * NK;
+            float s[NS][8];
+            if (a.len > 0) {
+#pragma unroll
+                for (int sb = 0; sb < NS; ++sb) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                        if constexpr (F8) {
+                            const float ks = pow2_of((ksr[sb][t] >> (8 * (n & 3))) & 255u);
+#pragma unroll
+                            for (int e = 0; e < ST; ++e) {
+                                u32x4 w;
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const unsigned u = kr[sb][t][e / 2][2 * (e & 1) + i];
+                                    w[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, ks, false));
+                                    w[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, ks, true));
+                                }
+#pragma unroll
+                                for (int i = QT - 1; i >= 0; --i)
+                                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                        __builtin_bit_cast(bf16x8, w), q[i][e], acc, 0, 0, 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < ST; ++e)
+#pragma unroll
+                                for (int i = QT - 1; i >= 0; --i)
+                                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                        __builtin_bit_cast(bf16x8, kr[sb][t][e]), q[i][e], acc, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[sb][4 * t + i] = acc[i] * c;
+                    }
+                }
+            }
+            if (more) {
+                load_keys(an, pgn);
+                if (x + 2 < x1) {
+                    ann = next(an);
+                    pgnn = load_pages(ann);
+                }
+            }
+            if (a.len > 0) {
+                if (!inside) {
+#pragma unroll
+                    for (int sb = 0; sb < NS; ++sb)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int key = key0 + 32 * sb + 8 * k4 + j;
+                            const bool out = key < a.start || key >= a.len;
+                            if (out) s[sb][j] = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < VW; ++i) vr[sb][j][i] = out ? 0u : vr[sb][j][i];
+                        }
+                }
+                float mx = s[0][0];
+#pragma unroll
+                for (int sb = 0; sb < NS; ++sb)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[sb][j]);
+                if (__any(mx > m + 8.f)) {
+                    const float mn = fmaxf(m, max_16_32(mx));
+                    const float al = __builtin_amdgcn_exp2f(m - mn);
+                    l *= al;
+#pragma unroll
+                    for (int i = 0; i < EV; ++i) o[i] *= al;
+                    m = mn;
+                }
+#pragma unroll
+                for (int sb = 0; sb < NS; ++sb) {
+                    float pr[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        pr[j] = __builtin_amdgcn_exp2f(s[sb][j] - m);
+                        l += pr[j];
+                    }
+                    if constexpr (F8) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float vs = pow2_of((vsr[sb][j / 4] >> (8 * (j & 3))) & 255u);
+                            if (!inside && s[sb][j] == -INFINITY) vs = 0.f;
+                            pr[j] *= vs;
+                        }
+                    }
+                    bf16x8 pt[PT];
+                    split_terms(pr, pt);
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) {
+                        constexpr int EW = F8 ? 4 : 2;   // elements per word
+                        u32x4 e[EW];   // element i of the word, positions in pairs
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const unsigned v0 = vr[sb][2 * j][w], v1 = vr[sb][2 * j + 1][w];
+                            if constexpr (F8) {
+                                const unsigned u0 = __builtin_amdgcn_perm(v1, v0, 0x05010400);
+                                const unsigned u1 = __builtin_amdgcn_perm(v1, v0, 0x07030602);
+                                e[0][j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u0, 1.f, false));
+                                e[1][j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u0, 1.f, true));
+                                e[2][j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u1, 1.f, false));
+                                e[3][j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u1, 1.f, true));
+                            } else {
+                                e[0][j] = __builtin_amdgcn_perm(v1, v0, 0x05040100);
+                                e[1][j] = __builtin_amdgcn_perm(v1, v0, 0x07060302);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < EW; ++i)
+#pragma unroll
+                            for (int t = PT - 1; t >= 0; --t)
+                                o[EW * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    __builtin_bit_cast(bf16x8, e[i]), pt[t], o[EW * w + i], 0, 0, 0);
+                    }
+                }
+            }
+            if (more) load_values(an, pgn);
+            const bool ends = a.t + 1 == a.nt;
+            if (ends || !more) {
+                // the unit's first tile, in the row of all
+                const int u0 = x - a.t;
+                if (bad) {
+                    l = __builtin_nanf("");
+                    if (lane == 0) flag_error(p.error, a.bad ? KL_DEVERR_POSITION : KL_DEVERR_PAGE);
+                }
+                const float L = sum_16_32(l);
+                const bool none = a.len == 0 && !bad;
+                if (ends && u0 >= first) {
+                    if (n < G) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int e = 0; e < EV; ++e) {
+                                const int dd = EV * (4 * k4 + i) + e;
+                                write_out(a.b, a.g, n, dd, o[e][i], m, none ? 1.f : L);
+                            }
+                    }
+                } else {
+                    const int slot = 2 * wave + (u0 >= first);
+                    if (n < G) {
+                        float *w = part + (slot * G + n) * WD;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int e = 0; e < EV; ++e) w[EV * (4 * k4 + i) + e] = o[e][i];
+                        if (k4 == 0) {
+                            w[D] = m;
+                            w[D + 1] = L;
+                        }
+                    }
+                    if (lane == 0) {
+                        unit[slot] = a.b * nkv + a.g;
+                        ubeg[slot] = u0;
+                        uend[slot] = u0 + a.nt;
+                    }
+                }
+                if (!more) break;
+                m = -INFINITY;
+                l = 0.f;
+                bad = false;
+#pragma unroll
+                for (int i = 0; i < EV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (an.len > 0) load_q(an);
+            }
+            ++x;
+            a = an;
+            pg = pgn;
+            bad = bad || a.bad || (a.len > 0 && page_bad);
+            an = ann;
+            pgn = pgnn;
+            more = x + 1 < x1;
+        }
+    }
     __syncthreads();
-    const float M = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
-    float L = 0.f;
-    for (int w = 0; w < 4; ++w) L += wl[w] * (wm[w] == -INFINITY && !isnan(wl[w]) ? 0.f : __expf(wm[w] - M));
-    if (isnan(wl[0]) || isnan(wl[1]) || isnan(wl[2]) || isnan(wl[3])) L = __builtin_nanf("");
-    for (int i = threadIdx.x; i < D; i += 256) {
-        float O = 0.f;
-        for (int w = 0; w < 4; ++w) O += wm[w] == -INFINITY ? 0.f : wo[w][i] * __expf(wm[w] - M);
-        store1(p.out, p.out_type, b * p.out_row + h * p.out_head + i, L == 0.f ? 0.f : O / L);
+
+    // join the parts in LDS, run by run of one unit's
+    // units handed on and their workgroups: one that began earlier, one that goes on
+    int sent0 = -1, sent1 = -1, count0 = 0, count1 = 0;
+    for (int e = 0; e < NE;) {
+        const int u = __builtin_amdgcn_readfirstlane(unit[e]);
+        if (u < 0) {
+            ++e;
+            continue;
+        }
+        int e1 = e + 1;
+        while (e1 < NE) {
+            const int v = __builtin_amdgcn_readfirstlane(unit[e1]);
+            if (v >= 0 && v != u) break;
+            ++e1;
+        }
+        const int b0 = __builtin_amdgcn_readfirstlane(ubeg[e]);
+        const int b1 = __builtin_amdgcn_readfirstlane(uend[e]);
+        const bool whole = b0 >= X0 && b1 <= X1;
+        const int z = b0 >= X0;
+        if (!whole) {
+            const int nw = share_of(T, np, b1 - 1) - share_of(T, np, b0) + 1;
+            if (z) sent1 = u, count1 = nw;
+            else sent0 = u, count0 = nw;
+        }
+        for (int i = tid; i < G * D; i += kAttnThreads) {
+            const int h = i / D, dd = i % D;
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            for (int k = e; k < e1; ++k)
+                if (unit[k] >= 0) M = fmaxf(M, part[(k * G + h) * WD + D]);
+            for (int k = e; k < e1; ++k) {
+                if (unit[k] < 0) continue;
+                const float *w = part + (k * G + h) * WD;
+                const float al = __builtin_amdgcn_exp2f(w[D] - M);
+                L = fmaf(w[D + 1], al, L);
+                O = fmaf(w[dd], al, O);
+            }
+            if (whole) {
+                write_out(u / nkv, u % nkv, h, dd, O, M, L);
+            } else {
+                float *w = p.parts + ((size_t)(wg * 2 + z) * G + h) * WD;
+                st_dev(w + dd, O);
+                if (dd == 0) {
+                    st_dev(w + D, M);
+                    st_dev(w + D + 1, L);
+                }
+            }
+        }
+        e = e1;
     }
-    if (p.lse && threadIdx.x == 0) p.lse[(long long)b * p.nq + h] = L == 0.f ? -INFINITY : M + logf(L);
+    if (sent0 < 0 && sent1 < 0) return;
+
+    // arrive with what was handed on; the last to arrive joins a unit's parts
+    wait_stores();
+    __syncthreads();
+    if (tid < 2) {
+        const int u = tid ? sent1 : sent0, nw = tid ? count1 : count0;
+        int mine = 0;
+        if (u >= 0)
+            mine = __hip_atomic_fetch_add(p.arrived + u, 1u, __ATOMIC_RELAXED,
+                                          __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(nw - 1);
+        if (mine)
+            __hip_atomic_store(p.arrived + u, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last[tid] = mine;
+    }
+    __syncthreads();
+    for (int z = 0; z < 2; ++z) {
+        if (!__builtin_amdgcn_readfirstlane(last[z])) continue;
+        const int u = z ? sent1 : sent0, nw = z ? count1 : count0;
+        const int b = u / nkv, g = u % nkv;
+        const int u0 = __builtin_amdgcn_readfirstlane(pre[b]) * nkv +
+                       g * __builtin_amdgcn_readfirstlane(pre[b + 1] - pre[b]);
+        const int f = share_of(T, np, u0);
+        for (int i = tid; i < G * D; i += kAttnThreads) {
+            const int h = i / D, dd = i % D;
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            auto src = [&](int k) {
+                return p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
+            };
+            constexpr int NB = 8;   // parts whose loads are issued together
+            for (int k0 = 0; k0 < nw; k0 += NB) {
+                float mm[NB], ll[NB], oo[NB], mn = M;
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    const float *w = src(min(k0 + k, nw - 1));
+                    mm[k] = ld_dev(w + D);
+                    ll[k] = ld_dev(w + D + 1);
+                    oo[k] = ld_dev(w + dd);
+                }
+#pragma unroll
+                for (int k = 0; k < NB; ++k) mn = k0 + k < nw ? fmaxf(mn, mm[k]) : mn;
+                const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+                L *= al;
+                O *= al;
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    if (k0 + k >= nw) continue;
+                    const float w = __builtin_amdgcn_exp2f(mm[k] - mn);
+                    L = fmaf(ll[k], w, L);
+                    O = fmaf(oo[k], w, O);
+                }
+                M = mn;
+            }
+            write_out(b, g, h, dd, O, M, L);
+        }
+    }
+}
+
+template <int D, bool F8, bool Full>
+static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
+    const auto kernel = kl_paged_attention_kernel<D, F8, Full>;
+    const int lds = 4 * (2 * kAttnWaves * (p.group * (D + 2) + 3) + kAttnWaves + 3 + p.t.batch + 1);
+    // (more than the default 64 KiB: once per device)
+    if (lds > 65536) {
+        static std::atomic<unsigned long long> done{0};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        const unsigned long long bit = 1ull << (dev & 63);
+        if (!(done.load(std::memory_order_relaxed) & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLdsMost);
+            if (e != hipSuccess) return e;
+            done.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    // at most a workgroup for every kAttnWaves tiles that the table has room for
+    const long long tiles = (((long long)p.t.max_pages << p.c.page_log2) + paged_tile(D, F8 ? 1 : 2) - 1) /
+                            paged_tile(D, F8 ? 1 : 2) * p.t.batch * p.c.nkv;
+    const int grid = (int)std::min<long long>((tiles + kAttnWaves - 1) / kAttnWaves, kPagedGroups);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kAttnThreads), lds, stream, p);
+    return hipGetLastError();
 }
 
 hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream) {
-    const dim3 grid(p.t.batch * p.nq);
-    if (p.c.d == 128)
-        hipLaunchKernelGGL(kl_paged_attention_kernel<128>, grid, dim3(256), 0, stream, p);
-    else
-        hipLaunchKernelGGL(kl_paged_attention_kernel<64>, grid, dim3(256), 0, stream, p);
-    return hipGetLastError();
+    const bool full = p.q_type != KL_DTYPE_BF16 || p.out_type == KL_DTYPE_FP32;
+    const int which = (p.c.d == 128 ? 4 : 0) + (p.c.e4m3 ? 2 : 0) + (full ? 1 : 0);
+    switch (which) {
+        case 0: return launch_attention<64, false, false>(p, stream);
+        case 1: return launch_attention<64, false, true>(p, stream);
+        case 2: return launch_attention<64, true, false>(p, stream);
+        case 3: return launch_attention<64, true, true>(p, stream);
+        case 4: return launch_attention<128, false, false>(p, stream);
+        case 5: return launch_attention<128, false, true>(p, stream);
+        case 6: return launch_attention<128, true, false>(p, stream);
+        default: return launch_attention<128, true, true>(p, stream);
+    }
 }
 
 }  // namespace kl

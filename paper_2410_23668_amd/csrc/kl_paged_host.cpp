@@ -49,8 +49,8 @@ kl_status check_pool(const kl_paged_cache *c, int32_t layer, const kl_page_table
     if (t->batch < 1 || t->max_pages < 1 || t->stride < t->max_pages)
         return fail(KL_ERR_INVALID_ARGUMENT, "%s: page table batch %d, max_pages %d, stride %d", who,
                     t->batch, t->max_pages, t->stride);
-    if ((int64_t)t->max_pages * c->page_size > INT32_MAX)
-        return fail(KL_ERR_UNSUPPORTED, "%s: max_pages * page_size above 2^31 - 1", who);
+    if ((int64_t)t->max_pages * c->page_size > (1 << 30))
+        return fail(KL_ERR_UNSUPPORTED, "%s: max_pages * page_size above 2^30", who);
     return KL_OK;
 }
 
@@ -166,7 +166,7 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch) 
              batch, kMaxPagedBatch);
         return 0;
     }
-    return 256;
+    return kPagedPartBytes + (size_t)batch * cache->n_kv_heads * sizeof(unsigned);
 }
 
 kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
@@ -191,6 +191,10 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     if (!lengths || !aligned(lengths, 4) || !aligned(lse, 4) || !aligned(error, 4))
         return fail(KL_ERR_INVALID_ARGUMENT, "%s: lengths must not be NULL, and int32/fp32 buffers "
                                              "4-byte aligned", who);
+    if ((int64_t)B * c.n_kv_heads * (((int64_t)table->max_pages * c.page_size + 31) / 32 + 1) >
+        INT32_MAX)
+        return fail(KL_ERR_UNSUPPORTED, "%s: batch * n_kv_heads * max_pages * page_size too large",
+                    who);
     st = check_rows(q, B, n_heads, c.head_dim, false, "q", who);
     if (st != KL_OK) return st;
     st = check_rows(out, B, n_heads, c.head_dim, true, "out", who);
@@ -207,10 +211,14 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     p.c = layer_of(c, layer); p.t = table_of(*table);
     p.lengths = lengths;
     p.q = q->data; p.q_type = q->dtype; p.q_row = q->row_stride; p.q_head = q->head_stride;
+    p.q_vec = vector_rows(*q, B, n_heads);
     p.out = out->data; p.out_type = out->dtype;
     p.out_row = out->row_stride; p.out_head = out->head_stride;
     p.nq = n_heads; p.group = n_heads / c.n_kv_heads;
     p.scale = scale; p.window = window; p.lse = lse; p.error = error;
+    p.parts = reinterpret_cast<float *>(workspace);
+    p.arrived = reinterpret_cast<unsigned *>(reinterpret_cast<uint8_t *>(workspace) +
+                                             kPagedPartBytes);
     HIP_TRY(launch_paged_attention(p, reinterpret_cast<hipStream_t>(stream)));
     return KL_OK;
 }

@@ -46,7 +46,7 @@ POOL = [
     (dict(t=table(pages=A + 2)), kb.KL_ERR_INVALID_ARGUMENT, "page table"),
     (dict(t=table(batch=0)), kb.KL_ERR_INVALID_ARGUMENT, "batch 0"),
     (dict(t=table(stride=4)), kb.KL_ERR_INVALID_ARGUMENT, "stride 4"),
-    (dict(t=table(max_pages=1 << 27, stride=1 << 27)), kb.KL_ERR_UNSUPPORTED, "2^31"),
+    (dict(t=table(max_pages=(1 << 26) + 1, stride=1 << 27)), kb.KL_ERR_UNSUPPORTED, "2^30"),
 ]
 ROWS = [
     (dict(pos=A + 1), kb.KL_ERR_INVALID_ARGUMENT, "4-byte"),

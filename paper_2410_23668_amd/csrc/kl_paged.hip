@@ -21,41 +21,43 @@ __device__ __forceinline__ float pow2_of(unsigned s) { return __uint_as_float(s 
 
 // ---------------------------------------------------------------- rows
 
-// 8 consecutive elements of a caller's row as floats, and back.
-__device__ __forceinline__ void load8(const void *p, int type, bool vec, float (&x)[8]) {
-    if (type == KL_DTYPE_FP32) {
-        const float *f = reinterpret_cast<const float *>(p);
-        if (vec) {
-            const f32x4 a = *reinterpret_cast<const f32x4 *>(f);
-            const f32x4 b = *reinterpret_cast<const f32x4 *>(f + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = a[i], x[i + 4] = b[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = f[i];
-        }
-        return;
-    }
-    unsigned u[4];
-    if (vec) {
-        const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = a[i];
-    } else {
-        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = h[2 * i] | ((unsigned)h[2 * i + 1] << 16);
-    }
+// 16 bytes of a caller's elements (16-bit ones, or floats), as one word where
+// it is aligned.
+template <class E>
+__device__ __forceinline__ u32x4 load_16B(const E *p, bool vec) {
+    if (vec) return *reinterpret_cast<const u32x4 *>(p);
+    u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (type == KL_DTYPE_BF16) {
-            x[2 * i] = bf_lo(u[i]);
-            x[2 * i + 1] = bf_hi(u[i]);
+        if constexpr (sizeof(E) == 4) w[i] = __builtin_bit_cast(unsigned, p[i]);
+        else w[i] = p[2 * i] | ((unsigned)p[2 * i + 1] << 16);
+    }
+    return w;
+}
+// 8 elements from their words (of 16-bit elements: the first four).
+__device__ __forceinline__ void words_to_f32(u32x4 a, u32x4 b, int type, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (type == KL_DTYPE_FP32) {
+            x[i] = __uint_as_float(a[i]);
+            x[i + 4] = __uint_as_float(b[i]);
+        } else if (type == KL_DTYPE_BF16) {
+            x[2 * i] = bf_lo(a[i]);
+            x[2 * i + 1] = bf_hi(a[i]);
         } else {
-            x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)u[i]);
-            x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[i] >> 16));
+            x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)a[i]);
+            x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(a[i] >> 16));
         }
     }
+}
+
+// 8 consecutive elements of a caller's row as floats, and back.
+__device__ __forceinline__ void load8(const void *p, int type, bool vec, float (&x)[8]) {
+    const float *f = reinterpret_cast<const float *>(p);
+    if (type == KL_DTYPE_FP32)
+        words_to_f32(load_16B(f, vec), load_16B(f + 4, vec), type, x);
+    else
+        words_to_f32(load_16B(reinterpret_cast<const uint16_t *>(p), vec), u32x4{}, type, x);
 }
 
 // The 16-bit pattern of x in type (bf16 or fp16), nearest even.
@@ -284,6 +286,27 @@ __device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
     }
 }
 
+// Adds the first n (at most NB) of the parts that get(j, output, maximum, sum)
+// reads, all of them at once, to (O, M, L).
+template <int NB, class Get>
+__device__ __forceinline__ void join_parts(int n, float &O, float &M, float &L, Get &&get) {
+    float o[NB], m[NB], l[NB], mn = M;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) get(j, o[j], m[j], l[j]);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) mn = j < n ? fmaxf(mn, m[j]) : mn;
+    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);   // (none yet: 0)
+    L *= a;
+    O *= a;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const float w = __builtin_amdgcn_exp2f(m[j] - mn);
+        L = j < n ? fmaf(l[j], w, L) : L;
+        O = j < n ? fmaf(o[j], w, O) : O;
+    }
+    M = mn;
+}
+
 template <int D, bool F8, bool Full>
 __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(AttnParams p) {
     constexpr int ES = F8 ? 1 : 2;
@@ -315,31 +338,49 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         bad = len < 0 || (long long)len > cap;
         return bad ? 0 : len;
     };
-    if (tid < NE) unit[tid] = -1;
-    if (tid == 0) pre[0] = 0;
-    int base = 0;
-    for (int b0 = 0; b0 < B; b0 += kAttnThreads) {
-        const int b = b0 + tid;
-        bool bad;
-        int s = b < B ? paged_tiles(length_of(b, bad), p.window, NK) : 0;
+    // Tiles of the sequences up to each: one per lane of every wave, where the
+    // wave has lanes for all (no wait for the other waves: 1 us less), else in LDS.
+    const bool few = B <= 64;
+    if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
+    int len_own = 0, upto = 0, T;
+    bool bad_own = false;
+    auto wave_scan = [&](int v) {   // inclusive sum over the lanes
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const int o = from_lane(s, max(lane - off, 0));
-            s += lane >= off ? o : 0;
+            const int o = from_lane(v, max(lane - off, 0));
+            v += lane >= off ? o : 0;
         }
-        if (lane == 63) wsum[wave] = s;
-        __syncthreads();
-        int add = base, all = 0;
+        return v;
+    };
+    if (few) {
+        if (lane < B) len_own = length_of(lane, bad_own);
+        upto = wave_scan(lane < B ? paged_tiles(len_own, p.window, NK) : 0);
+        T = __builtin_amdgcn_readlane(upto, 63) * nkv;
+    } else {
+        if (tid == 0) pre[0] = 0;
+        int base = 0;
+        for (int b0 = 0; b0 < B; b0 += kAttnThreads) {
+            const int b = b0 + tid;
+            bool bad;
+            const int s = wave_scan(b < B ? paged_tiles(length_of(b, bad), p.window, NK) : 0);
+            if (lane == 63) wsum[wave] = s;
+            __syncthreads();
+            int add = base;
 #pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) {
-            if (w < wave) add += wsum[w];
-            all += wsum[w];
+            for (int w = 0; w < kAttnWaves; ++w) {
+                if (w < wave) add += wsum[w];
+                base += wsum[w];
+            }
+            if (b < B) pre[b + 1] = add + s;
+            __syncthreads();
         }
-        if (b < B) pre[b + 1] = add + s;
-        base += all;
-        __syncthreads();
+        T = __builtin_amdgcn_readfirstlane(base) * nkv;
     }
-    const int T = __builtin_amdgcn_readfirstlane(base) * nkv;
+    // tiles (of one KV head) of the sequences before b
+    auto before = [&](int b) {
+        if (few) return b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+        return __builtin_amdgcn_readfirstlane(pre[b]);
+    };
     // (a workgroup for every kAttnWaves tiles, so that each wave has one)
     const int np = min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves);
     const int wg = blockIdx.x;
@@ -358,21 +399,30 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     };
     auto enter = [&](At &a, int b) {
         a.b = b;
-        a.nt = __builtin_amdgcn_readfirstlane(pre[b + 1] - pre[b]);
-        a.len = __builtin_amdgcn_readfirstlane(length_of(b, a.bad));
+        a.nt = before(b + 1) - before(b);
+        if (few) {
+            a.len = __builtin_amdgcn_readlane(len_own, b);
+            a.bad = __builtin_amdgcn_readlane((int)bad_own, b) != 0;
+        } else {
+            a.len = __builtin_amdgcn_readfirstlane(length_of(b, a.bad));
+        }
         a.start = paged_start(a.len, p.window);
         a.t0 = paged_first_tile(a.len, p.window, NK);
     };
     auto find = [&](int i) {
-        int lo = 0, hi = B;   // pre[lo] nkv <= i < pre[hi] nkv
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (__builtin_amdgcn_readfirstlane(pre[mid]) * nkv <= i) lo = mid;
-            else hi = mid;
+        int lo = 0;   // before(lo) nkv <= i < before(lo + 1) nkv
+        if (few) {
+            lo = __popcll(__ballot(lane < B && upto * nkv <= i));
+        } else {
+            for (int hi = B; hi - lo > 1;) {
+                const int mid = (lo + hi) >> 1;
+                if (before(mid) * nkv <= i) lo = mid;
+                else hi = mid;
+            }
         }
         At a;
         enter(a, lo);
-        const int r = i - __builtin_amdgcn_readfirstlane(pre[lo]) * nkv;
+        const int r = i - before(lo) * nkv;
         a.g = r / a.nt;
         a.t = r % a.nt;
         return a;
@@ -466,23 +516,44 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         }
     };
 
+    // The queries of a unit as columns of the first product: asked for as they
+    // are, and taken apart into terms when they are needed.
+    constexpr int QW = Full ? 2 : 1;   // 16-byte words of 8 elements, at most
     bf16x8 q[QT][ST];
-    auto load_q = [&](const At &a) {
+    auto ask_q = [&](const At &a, u32x4 (&raw)[ST][QW]) {
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
             const int d0 = F8 ? 64 * (s / 2) + 16 * k4 + 8 * (s & 1) : 32 * s + 8 * k4;
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-            if (n < G) {
-                const long long at = a.b * p.q_row + (a.g * G + n) * p.q_head + d0;
-                load8(reinterpret_cast<const uint8_t *>(p.q) + at * (p.q_type == KL_DTYPE_FP32 ? 4 : 2),
-                      p.q_type, p.q_vec, v);
+            // (columns past the group: head 0 again, masked below)
+            const long long at = a.b * p.q_row + (a.g * G + (n < G ? n : 0)) * p.q_head + d0;
+            const float *f = reinterpret_cast<const float *>(p.q) + at;
+            if (Full && p.q_type == KL_DTYPE_FP32) {
+                raw[s][0] = load_16B(f, p.q_vec);
+                raw[s][QW - 1] = load_16B(f + 4, p.q_vec);
+            } else {
+                raw[s][0] = load_16B(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
+                if (Full) raw[s][QW - 1] = raw[s][0];
             }
-            bf16x8 t[QT];
-            split_terms(v, t);
+        }
+    };
+    auto take_q = [&](const u32x4 (&raw)[ST][QW]) {
 #pragma unroll
-            for (int i = 0; i < QT; ++i) q[i][s] = t[i];
+        for (int s = 0; s < ST; ++s) {
+            if constexpr (Full) {
+                float v[8];
+                words_to_f32(raw[s][0], raw[s][QW - 1], p.q_type, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = n < G ? v[j] : 0.f;
+                bf16x8 t[QT];
+                split_terms(v, t);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) q[i][s] = t[i];
+            } else {   // (bf16 queries are their own term)
+                u32x4 w = raw[s][0];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = n < G ? w[i] : 0u;
+                q[0][s] = __builtin_bit_cast(bf16x8, w);
+            }
         }
     };
 
@@ -504,10 +575,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             an = next(a);
             pgn = load_pages(an);
         }
-        load_keys(a, pg);
+        {
+            u32x4 raw[ST][QW];
+            ask_q(a, raw);
+            load_keys(a, pg);
+            load_values(a, pg);
+            take_q(raw);
+        }
         bool bad = a.bad || (a.len > 0 && page_bad);
-        load_values(a, pg);
-        load_q(a);
         float m = -INFINITY, l = 0.f;
         f32x4 o[EV];
 #pragma unroll
@@ -640,35 +715,32 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                     if (lane == 0) flag_error(p.error, a.bad ? KL_DEVERR_POSITION : KL_DEVERR_PAGE);
                 }
                 const float L = sum_16_32(l);
-                const bool none = a.len == 0 && !bad;
-                if (ends && u0 >= first) {
-                    if (n < G) {
+                // into LDS: a unit's part, or a whole unit on its way out (in
+                // the place of the part that the wave may end with)
+                const bool whole = ends && u0 >= first;
+                const int slot = 2 * wave + (u0 >= first);
+                float *const w = part + slot * G * WD;
+                if (n < G) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                            for (int e = 0; e < EV; ++e) {
-                                const int dd = EV * (4 * k4 + i) + e;
-                                write_out(a.b, a.g, n, dd, o[e][i], m, none ? 1.f : L);
-                            }
+                        for (int e = 0; e < EV; ++e) w[n * WD + EV * (4 * k4 + i) + e] = o[e][i];
+                    if (k4 == 0) {
+                        w[n * WD + D] = m;
+                        w[n * WD + D + 1] = a.len == 0 && !bad ? 1.f : L;
                     }
-                } else {
-                    const int slot = 2 * wave + (u0 >= first);
-                    if (n < G) {
-                        float *w = part + (slot * G + n) * WD;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int e = 0; e < EV; ++e) w[EV * (4 * k4 + i) + e] = o[e][i];
-                        if (k4 == 0) {
-                            w[D] = m;
-                            w[D + 1] = L;
-                        }
+                }
+                if (whole) {
+                    __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses are in order)
+                    for (int i = lane; i < G * D; i += 64) {
+                        const int h = i / D;
+                        write_out(a.b, a.g, h, i % D, w[h * WD + i % D], w[h * WD + D],
+                                  w[h * WD + D + 1]);
                     }
-                    if (lane == 0) {
-                        unit[slot] = a.b * nkv + a.g;
-                        ubeg[slot] = u0;
-                        uend[slot] = u0 + a.nt;
-                    }
+                } else if (lane == 0) {
+                    unit[slot] = a.b * nkv + a.g;
+                    ubeg[slot] = u0;
+                    uend[slot] = u0 + a.nt;
                 }
                 if (!more) break;
                 m = -INFINITY;
@@ -676,7 +748,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 bad = false;
 #pragma unroll
                 for (int i = 0; i < EV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (an.len > 0) load_q(an);
+                if (an.len > 0) {
+                    u32x4 raw[ST][QW];
+                    ask_q(an, raw);
+                    take_q(raw);
+                }
             }
             ++x;
             a = an;
@@ -689,21 +765,16 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     }
     __syncthreads();
 
-    // join the parts in LDS, run by run of one unit's
+    // join the parts in LDS, run by run of one unit's (lane i: part i)
     // units handed on and their workgroups: one that began earlier, one that goes on
     int sent0 = -1, sent1 = -1, count0 = 0, count1 = 0;
-    for (int e = 0; e < NE;) {
-        const int u = __builtin_amdgcn_readfirstlane(unit[e]);
-        if (u < 0) {
-            ++e;
-            continue;
-        }
-        int e1 = e + 1;
-        while (e1 < NE) {
-            const int v = __builtin_amdgcn_readfirstlane(unit[e1]);
-            if (v >= 0 && v != u) break;
-            ++e1;
-        }
+    const int own_unit = lane < NE ? unit[lane] : -1;
+    unsigned left = (unsigned)__ballot(own_unit >= 0);
+    while (left) {
+        const int e = __builtin_ctz(left);
+        const int u = __builtin_amdgcn_readlane(own_unit, e);
+        const unsigned run = (unsigned)__ballot(own_unit == u);
+        left &= ~run;
         const int b0 = __builtin_amdgcn_readfirstlane(ubeg[e]);
         const int b1 = __builtin_amdgcn_readfirstlane(uend[e]);
         const bool whole = b0 >= X0 && b1 <= X1;
@@ -715,15 +786,22 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         }
         for (int i = tid; i < G * D; i += kAttnThreads) {
             const int h = i / D, dd = i % D;
+            constexpr int NB = 8;   // parts read together (a run has 9 at most)
             float M = -INFINITY, L = 0.f, O = 0.f;
-            for (int k = e; k < e1; ++k)
-                if (unit[k] >= 0) M = fmaxf(M, part[(k * G + h) * WD + D]);
-            for (int k = e; k < e1; ++k) {
-                if (unit[k] < 0) continue;
-                const float *w = part + (k * G + h) * WD;
-                const float al = __builtin_amdgcn_exp2f(w[D] - M);
-                L = fmaf(w[D + 1], al, L);
-                O = fmaf(w[dd], al, O);
+            for (unsigned r = run; r;) {
+                int k[NB], nk = 0;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    k[j] = r ? __builtin_ctz(r) : e;
+                    nk += r != 0;
+                    r &= r - 1;
+                }
+                join_parts<NB>(nk, O, M, L, [&](int j, float &o, float &m, float &l) {
+                    const float *w = part + (k[j] * G + h) * WD;
+                    m = w[D];
+                    l = w[D + 1];
+                    o = w[dd];
+                });
             }
             if (whole) {
                 write_out(u / nkv, u % nkv, h, dd, O, M, L);
@@ -736,7 +814,6 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 }
             }
         }
-        e = e1;
     }
     if (sent0 < 0 && sent1 < 0) return;
 
@@ -758,39 +835,19 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         if (!__builtin_amdgcn_readfirstlane(last[z])) continue;
         const int u = z ? sent1 : sent0, nw = z ? count1 : count0;
         const int b = u / nkv, g = u % nkv;
-        const int u0 = __builtin_amdgcn_readfirstlane(pre[b]) * nkv +
-                       g * __builtin_amdgcn_readfirstlane(pre[b + 1] - pre[b]);
-        const int f = share_of(T, np, u0);
+        const int f = share_of(T, np, before(b) * nkv + g * (before(b + 1) - before(b)));
         for (int i = tid; i < G * D; i += kAttnThreads) {
             const int h = i / D, dd = i % D;
+            constexpr int NB = 16;   // parts whose loads are issued together
             float M = -INFINITY, L = 0.f, O = 0.f;
-            auto src = [&](int k) {
-                return p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
-            };
-            constexpr int NB = 8;   // parts whose loads are issued together
-            for (int k0 = 0; k0 < nw; k0 += NB) {
-                float mm[NB], ll[NB], oo[NB], mn = M;
-#pragma unroll
-                for (int k = 0; k < NB; ++k) {
-                    const float *w = src(min(k0 + k, nw - 1));
-                    mm[k] = ld_dev(w + D);
-                    ll[k] = ld_dev(w + D + 1);
-                    oo[k] = ld_dev(w + dd);
-                }
-#pragma unroll
-                for (int k = 0; k < NB; ++k) mn = k0 + k < nw ? fmaxf(mn, mm[k]) : mn;
-                const float al = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-                L *= al;
-                O *= al;
-#pragma unroll
-                for (int k = 0; k < NB; ++k) {
-                    if (k0 + k >= nw) continue;
-                    const float w = __builtin_amdgcn_exp2f(mm[k] - mn);
-                    L = fmaf(ll[k], w, L);
-                    O = fmaf(oo[k], w, O);
-                }
-                M = mn;
-            }
+            for (int k0 = 0; k0 < nw; k0 += NB)
+                join_parts<NB>(nw - k0, O, M, L, [&](int j, float &o, float &m, float &l) {
+                    const int k = min(k0 + j, nw - 1);
+                    const float *w = p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
+                    m = ld_dev(w + D);
+                    l = ld_dev(w + D + 1);
+                    o = ld_dev(w + dd);
+                });
             write_out(b, g, h, dd, O, M, L);
         }
     }

@@ -54,7 +54,7 @@ struct AttnParams {
     const void *q;
     void *out;
     int q_type, out_type, nq, group;
-    bool q_vec;                      // as k_vec
+    bool q_vec, out_vec;             // as k_vec
     long long q_row, q_head, out_row, out_head;
     float scale;
     int window;

@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     // wave has lanes for all (no wait for the other waves: 1 us less), else in LDS.
     const bool few = B <= 64;
     if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
-    int len_own = 0, upto = 0, T;
+    int len_own = 0, upto = 0, most = 0, T;
     bool bad_own = false;
     auto wave_scan = [&](int v) {   // inclusive sum over the lanes
 #pragma unroll
@@ -354,7 +354,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     };
     if (few) {
         if (lane < B) len_own = length_of(lane, bad_own);
-        upto = wave_scan(lane < B ? paged_tiles(len_own, p.window, NK) : 0);
+        const int own = lane < B ? paged_tiles(len_own, p.window, NK) : 0;
+        upto = wave_scan(own);
+        most = (int)wave_max((float)own);   // (below 2^24: cap and NK)
         T = __builtin_amdgcn_readlane(upto, 63) * nkv;
     } else {
         if (tid == 0) pre[0] = 0;
@@ -381,15 +383,23 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         if (few) return b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
         return __builtin_amdgcn_readfirstlane(pre[b]);
     };
-    // (a workgroup for every kAttnWaves tiles, so that each wave has one)
-    const int np = min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves);
+    // the workgroup's share [X0, X1): a unit of its own (unit_shares), or an
+    // equal share, with a workgroup for every kAttnWaves tiles
     const int wg = blockIdx.x;
-    if (wg >= np) return;
-    const int X0 = share_first(T, np, wg), X1 = share_first(T, np, wg + 1);
-    int x, x1;
-    split_range(X1 - X0, kAttnWaves, wave, x, x1);
-    x += X0;
-    x1 += X0;
+    const bool by_unit = few && unit_shares(B * nkv, gridDim.x, most, T, kAttnWaves);
+    const Shares sh(T, by_unit ? B * nkv : min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves));
+    if (wg >= sh.np) return;
+    int X0, X1;
+    if (by_unit) {
+        const int b = wg / nkv, g = wg % nkv, nt = before(b + 1) - before(b);
+        X0 = before(b) * nkv + g * nt;
+        X1 = X0 + nt;
+    } else {
+        X0 = sh.first(wg);
+        X1 = sh.first(wg + 1);
+    }
+    int x = X0 + (((X1 - X0) * wave) / kAttnWaves);
+    const int x1 = X0 + (((X1 - X0) * (wave + 1)) / kAttnWaves);
 
     // A place in the row of tiles.
     struct At {
@@ -465,54 +475,77 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         page_bad = __any((unsigned)pages >= (unsigned)p.c.n_pages);
         if ((unsigned)pages >= (unsigned)p.c.n_pages) pages = 0;
         const int key0 = (a.t0 + a.t) * NK;
-        const bool inside = tile_inside(a);
+        if (tile_inside(a)) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int key = key0 + 32 * s + 8 * (n >> 2);
+                const long long r0 = page_row(a, pages, 4 * s + (n >> 2)) + (key & psm);
+                const uint8_t *src = p.c.k + (r0 + (n & 3)) * RB + 16 * k4;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) kr[s][t][c] = ld_stream_16B(src + 4 * t * RB + 64 * c);
+                if constexpr (F8) ksr[s] = *reinterpret_cast<const u32x2 *>(p.c.ks + r0);
+            }
+            return;
+        }
+        // (rows outside the attended positions: the nearest attended one's)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int gk = key0 + 32 * s + 8 * (n >> 2);
             const long long r0 = page_row(a, pages, 4 * s + (n >> 2));
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                int key = gk + 4 * t + (n & 3);
-                if (!inside) key = min(max(key, a.start), a.len - 1);
+                const int key = min(max(gk + 4 * t + (n & 3), a.start), a.len - 1);
                 const uint8_t *src = p.c.k + (r0 + (key & psm)) * RB + 16 * k4;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) kr[s][t][c] = ld_stream_16B(src + 64 * c);
             }
-            if constexpr (F8) {
-                const int grp = inside ? gk : min(max(gk, a.start), a.len - 1) & ~7;
-                ksr[s] = *reinterpret_cast<const u32x2 *>(p.c.ks + r0 + (grp & psm));
-            }
+            if constexpr (F8)
+                ksr[s] = *reinterpret_cast<const u32x2 *>(
+                    p.c.ks + r0 + (min(max(gk, a.start), a.len - 1) & psm & ~7));
+        }
+    };
+    auto load_value = [&](const uint8_t *src, unsigned (&v)[VW]) {
+        if constexpr (VW == 4) {
+            const u32x4 w = ld_stream_16B(src);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = w[i];
+        } else if constexpr (VW == 2) {
+            const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(src));
+            v[0] = w[0];
+            v[1] = w[1];
+        } else {
+            v[0] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(src));
         }
     };
     auto load_values = [&](const At &a, int pages) {
         if (a.len == 0) return;
         const int key0 = (a.t0 + a.t) * NK;
-        const bool inside = tile_inside(a);
+        if (tile_inside(a)) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int key = key0 + 32 * s + 8 * k4;
+                const long long r0 = page_row(a, pages, 4 * s + k4) + (key & psm);
+                const uint8_t *src = p.c.v + r0 * RB + n * (EV * ES);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) load_value(src + j * RB, vr[s][j]);
+                if constexpr (F8) vsr[s] = *reinterpret_cast<const u32x2 *>(p.c.vs + r0);
+            }
+            return;
+        }
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int gk = key0 + 32 * s + 8 * k4;
             const long long r0 = page_row(a, pages, 4 * s + k4);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                int key = gk + j;
-                if (!inside) key = min(max(key, a.start), a.len - 1);
-                const uint8_t *src = p.c.v + (r0 + (key & psm)) * RB + n * (EV * ES);
-                if constexpr (VW == 4) {
-                    const u32x4 w = ld_stream_16B(src);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) vr[s][j][i] = w[i];
-                } else if constexpr (VW == 2) {
-                    const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(src));
-                    vr[s][j][0] = w[0];
-                    vr[s][j][1] = w[1];
-                } else {
-                    vr[s][j][0] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(src));
-                }
+                const int key = min(max(gk + j, a.start), a.len - 1);
+                load_value(p.c.v + (r0 + (key & psm)) * RB + n * (EV * ES), vr[s][j]);
             }
-            if constexpr (F8) {
-                const int grp = inside ? gk : min(max(gk, a.start), a.len - 1) & ~7;
-                vsr[s] = *reinterpret_cast<const u32x2 *>(p.c.vs + r0 + (grp & psm));
-            }
+            if constexpr (F8)
+                vsr[s] = *reinterpret_cast<const u32x2 *>(
+                    p.c.vs + r0 + (min(max(gk, a.start), a.len - 1) & psm & ~7));
         }
     };
 
@@ -536,6 +569,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             }
         }
     };
+    const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
     auto take_q = [&](const u32x4 (&raw)[ST][QW]) {
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
@@ -543,7 +577,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 float v[8];
                 words_to_f32(raw[s][0], raw[s][QW - 1], p.q_type, v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = n < G ? v[j] : 0.f;
+                for (int j = 0; j < 8; ++j) v[j] = n < G ? v[j] * sign : 0.f;
                 bf16x8 t[QT];
                 split_terms(v, t);
 #pragma unroll
@@ -551,22 +585,28 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             } else {   // (bf16 queries are their own term)
                 u32x4 w = raw[s][0];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = n < G ? w[i] : 0u;
+                for (int i = 0; i < 4; ++i)
+                    w[i] = n < G && sign != 0.f ? w[i] ^ (sign < 0.f ? 0x80008000u : 0u) : 0u;
                 q[0][s] = __builtin_bit_cast(bf16x8, w);
             }
         }
     };
 
-    // output i = element dd of query head h of the group: O unnormalised, M
-    // the maximum (log2 units), L the sum
+    const int out_bytes = p.out_type == KL_DTYPE_FP32 ? 4 : 2;
+    // head h of the group, of maximum M (log2 units) and sum L
+    auto write_lse = [&](int b, int g, int h, float M, float L) {
+        p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
+    };
+    // its element dd, O unnormalised
     auto write_out = [&](int b, int g, int h, int dd, float O, float M, float L) {
         store1(p.out, p.out_type, b * p.out_row + (g * G + h) * p.out_head + dd, O / L);
-        if (p.lse && dd == 0)
-            p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
+        if (p.lse && dd == 0) write_lse(b, g, h, M, L);
     };
 
     if (x < x1) {
-        const float c = p.scale * 1.4426950408889634f;
+        // scores are c S^T in log2 units, c > 0: a negative scale's sign is in
+        // the queries, as is a zero scale
+        const float c = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.4426950408889634f;
         const int first = x;
         At a = find(x), an, ann;
         int pg = load_pages(a), pgn = 0, pgnn = 0;
@@ -622,7 +662,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                                         __builtin_bit_cast(bf16x8, kr[sb][t][e]), q[i][e], acc, 0, 0, 0);
                         }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[sb][4 * t + i] = acc[i] * c;
+                        for (int i = 0; i < 4; ++i) s[sb][4 * t + i] = acc[i];
                     }
                 }
             }
@@ -651,6 +691,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 for (int sb = 0; sb < NS; ++sb)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[sb][j]);
+                mx *= c;
                 if (__any(mx > m + 8.f)) {
                     const float mn = fmaxf(m, max_16_32(mx));
                     const float al = __builtin_amdgcn_exp2f(m - mn);
@@ -664,7 +705,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                     float pr[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        pr[j] = __builtin_amdgcn_exp2f(s[sb][j] - m);
+                        pr[j] = __builtin_amdgcn_exp2f(fmaf(s[sb][j], c, -m));
                         l += pr[j];
                     }
                     if constexpr (F8) {
@@ -732,10 +773,17 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 }
                 if (whole) {
                     __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses are in order)
-                    for (int i = lane; i < G * D; i += 64) {
-                        const int h = i / D;
-                        write_out(a.b, a.g, h, i % D, w[h * WD + i % D], w[h * WD + D],
-                                  w[h * WD + D + 1]);
+                    for (int i = 8 * lane; i < G * D; i += 512) {
+                        const int h = i / D, dd = i % D;
+                        const float *const r = w + h * WD;
+                        const float inv = 1.f / r[D + 1];
+                        float v[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = r[dd + j] * inv;
+                        store8(reinterpret_cast<uint8_t *>(p.out) +
+                                   (a.b * p.out_row + (a.g * G + h) * p.out_head + dd) * out_bytes,
+                               p.out_type, p.out_vec, v);
+                        if (p.lse && dd == 0) write_lse(a.b, a.g, h, r[D], r[D + 1]);
                     }
                 } else if (lane == 0) {
                     unit[slot] = a.b * nkv + a.g;
@@ -780,7 +828,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         const bool whole = b0 >= X0 && b1 <= X1;
         const int z = b0 >= X0;
         if (!whole) {
-            const int nw = share_of(T, np, b1 - 1) - share_of(T, np, b0) + 1;
+            const int nw = sh.of(b1 - 1) - sh.of(b0) + 1;
             if (z) sent1 = u, count1 = nw;
             else sent0 = u, count0 = nw;
         }
@@ -835,7 +883,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         if (!__builtin_amdgcn_readfirstlane(last[z])) continue;
         const int u = z ? sent1 : sent0, nw = z ? count1 : count0;
         const int b = u / nkv, g = u % nkv;
-        const int f = share_of(T, np, before(b) * nkv + g * (before(b + 1) - before(b)));
+        const int f = sh.of(before(b) * nkv + g * (before(b + 1) - before(b)));
         for (int i = tid; i < G * D; i += kAttnThreads) {
             const int h = i / D, dd = i % D;
             constexpr int NB = 16;   // parts whose loads are issued together
@@ -874,7 +922,10 @@ static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
     // at most a workgroup for every kAttnWaves tiles that the table has room for
     const long long tiles = (((long long)p.t.max_pages << p.c.page_log2) + paged_tile(D, F8 ? 1 : 2) - 1) /
                             paged_tile(D, F8 ? 1 : 2) * p.t.batch * p.c.nkv;
-    const int grid = (int)std::min<long long>((tiles + kAttnWaves - 1) / kAttnWaves, kPagedGroups);
+    // (or for every unit)
+    const int grid = (int)std::min<long long>(
+        std::max<long long>((tiles + kAttnWaves - 1) / kAttnWaves, (long long)p.t.batch * p.c.nkv),
+        kPagedGroups);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(kAttnThreads), lds, stream, p);
     return hipGetLastError();
 }

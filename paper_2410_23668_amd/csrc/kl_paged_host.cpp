@@ -212,6 +212,7 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     p.lengths = lengths;
     p.q = q->data; p.q_type = q->dtype; p.q_row = q->row_stride; p.q_head = q->head_stride;
     p.q_vec = vector_rows(*q, B, n_heads);
+    p.out_vec = vector_rows(*out, B, n_heads);
     p.out = out->data; p.out_type = out->dtype;
     p.out_row = out->row_stride; p.out_head = out->head_stride;
     p.nq = n_heads; p.group = n_heads / c.n_kv_heads;

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkl.so")
 SOURCES = [os.path.join(CSRC, f) for f in (
     "kl_step_d128.hip", "kl_step_d128_batched.hip", "kl_step_d64.hip", "kl_step_d64_batched.hip",
-    "kl_device.hip", "kl_paged.hip", "kl_host.cpp", "kl_paged_host.cpp")]
+    "kl_device.hip", "kl_paged.hip", "kl_paged_d64.hip", "kl_paged_d128.hip", "kl_host.cpp",
+    "kl_paged_host.cpp")]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

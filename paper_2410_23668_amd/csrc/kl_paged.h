@@ -64,5 +64,7 @@ struct AttnParams {
     int32_t *error;
 };
 hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream);
+hipError_t launch_paged_attention_d64(const AttnParams &p, hipStream_t stream);
+hipError_t launch_paged_attention_d128(const AttnParams &p, hipStream_t stream);
 
 }  // namespace kl

@@ -1,0 +1,779 @@
+// The paged cache's attention kernel (kl_paged_attention in include/kl.h),
+// included by the translation units that instantiate it (kl_paged_d*.hip).
+#pragma once
+
+#include <algorithm>
+#include <atomic>
+
+#include "kl_paged_dev.h"
+#include "kl_paged_shares.h"
+
+namespace kl {
+
+// Split-K flash decoding over pages.  A unit is a (sequence, KV head); its
+// attended positions are cut into tiles of 16 KiB of keys and values, and the
+// tiles of all units, one unit after the other, are dealt in equal contiguous
+// shares to the workgroups and within one to its eight waves, so that lengths
+// of any kind load every wave alike.  A wave goes through its tiles with a
+// running maximum and sum; a unit that lies inside its share it writes out,
+// of a unit cut by the share's ends it leaves its part (maximum, sum,
+// unnormalised output) in LDS.  The workgroup joins the parts there; what is
+// part of a unit of several workgroups goes to the workspace, and the last of
+// them to arrive (a counter per unit) joins all in workgroup order.
+//
+// All query heads of a KV head share one pass over its keys and values on the
+// matrix cores, in layouts that need no exchange between lanes:
+//   S^T = K Q^T  v_mfma_f32_16x16x32_bf16: A = 16 key rows, B = the queries as
+//                columns.  The rows of two such products, t = 0 and 1, are the
+//                positions 8 (r / 4) + 4 t + r % 4 of a block of 32, so that
+//                lane (k4, n) ends up with the scores of head n and positions
+//                8 k4 .. 8 k4 + 7: what the second product wants of it.
+//   O^T = V^T P^T  A = V^T: lane (k4, r) has loaded elements EV r .. EV r +
+//                EV - 1 (EV = d / 16) of the 8 positions, one load a position
+//                that covers the whole row; product m takes element m of each,
+//                pairs of positions put together by byte permutes.
+// A group of up to 8 or 4 heads has its columns 2 or 4 times (column n: head
+// n % (16 / C), copy n / (16 / C)), which costs the products nothing: each copy
+// goes on with its own 8 / C of the lane's 8 scores, so that the softmax's
+// vector instructions are spent on a fourth of what 16 columns would need,
+// and the copies' outputs are added at the unit's end.
+// e4m3 rows become bf16 (exactly) on the way, keys with their row's scale,
+// values without: theirs goes into the probabilities.  Queries of 32 or 16
+// bits that bf16 cannot hold, and the probabilities, are taken as several bf16
+// terms: three are all 24 bits of a float; two, 16 bits, where the output has
+// 16 bits (the weights are off by 2^-17, an eighth of its fp16 half-step at
+// most).  Softmax and sums are fp32; the maximum moves only when a score passes
+// it by 2^8, so the loop has no cross-lane step.
+
+constexpr int kAttnWaves = 8;
+constexpr int kAttnThreads = kAttnWaves * 64;
+
+__device__ __forceinline__ float load1(const void *p, int type, long long i) {
+    if (type == KL_DTYPE_FP32) return reinterpret_cast<const float *>(p)[i];
+    const uint16_t h = reinterpret_cast<const uint16_t *>(p)[i];
+    return type == KL_DTYPE_BF16 ? bf2f(h) : (float)__builtin_bit_cast(_Float16, h);
+}
+__device__ __forceinline__ void store1(void *p, int type, long long i, float x) {
+    if (type == KL_DTYPE_FP32) reinterpret_cast<float *>(p)[i] = x;
+    else reinterpret_cast<uint16_t *>(p)[i] = bits16(x, type);
+}
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(unsigned, v);
+}
+// NT bf16 terms of 8 floats (x is left as what the terms do not hold)
+template <int NT>
+__device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+            if (i + 1 < NT) {
+                x[2 * j] -= bf_lo(w[j]);
+                x[2 * j + 1] -= bf_hi(w[j]);
+            }
+        }
+        t[i] = __builtin_bit_cast(bf16x8, w);
+    }
+}
+
+// Adds the first n (at most NB) of the parts that get(j, output, maximum, sum)
+// reads, all of them at once, to (O, M, L).
+template <int NB, class Get>
+__device__ __forceinline__ void join_parts(int n, float &O, float &M, float &L, Get &&get) {
+    float o[NB], m[NB], l[NB], mn = M;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) get(j, o[j], m[j], l[j]);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) mn = j < n ? fmaxf(mn, m[j]) : mn;
+    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);   // (none yet: 0)
+    L *= a;
+    O *= a;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const float w = __builtin_amdgcn_exp2f(m[j] - mn);
+        L = j < n ? fmaf(l[j], w, L) : L;
+        O = j < n ? fmaf(o[j], w, O) : O;
+    }
+    M = mn;
+}
+
+// Scale bytes of N consecutive positions, and the i-th.
+template <int N> struct ScaleWord;
+template <> struct ScaleWord<8> { typedef u32x2 type; };
+template <> struct ScaleWord<4> { typedef unsigned type; };
+template <> struct ScaleWord<2> { typedef uint16_t type; };
+__device__ __forceinline__ unsigned scale_byte(u32x2 w, int i) { return (w[i / 4] >> (8 * (i & 3))) & 255u; }
+__device__ __forceinline__ unsigned scale_byte(unsigned w, int i) { return (w >> (8 * i)) & 255u; }
+
+// without the i-th
+__device__ __forceinline__ void clear_scale(u32x2 &w, int i) { w[i / 4] &= ~(255u << (8 * (i & 3))); }
+__device__ __forceinline__ void clear_scale(unsigned &w, int i) { w &= ~(255u << (8 * i)); }
+__device__ __forceinline__ void clear_scale(uint16_t &w, int i) { w &= (uint16_t)~(255u << (8 * i)); }
+
+// Two of a word's four e4m3 codes (the upper two: Hi) as bf16, times a power of two.
+template <bool Hi>
+__device__ __forceinline__ unsigned fp8_to_bf16(unsigned w, float scale) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, Hi));
+}
+
+// op over the C columns (of 16) that a head has; every one of them gets it.
+struct MaxOp { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct AddOp { __device__ float operator()(float a, float b) const { return a + b; } };
+template <int C, class Op>
+__device__ __forceinline__ float over_copies(float v, Op op) {
+    if constexpr (C >= 2) v = op(v, dpp<0x128>(v));   // row_ror:8
+    if constexpr (C >= 4) v = op(v, dpp<0x124>(v));   // row_ror:4
+    return v;
+}
+
+template <int D, bool F8, bool Full, int C>
+__global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(AttnParams p) {
+    constexpr int ES = F8 ? 1 : 2;
+    constexpr int NK = paged_tile(D, ES), NS = NK / 32;   // positions of a tile; blocks of 32
+    constexpr int RB = D * ES;                  // bytes of a row
+    constexpr int NC = RB / 64;                 // 16-byte loads of a key row per lane
+    constexpr int EV = D / 16, VW = EV * ES / 4;   // value elements, words per lane and position
+    constexpr int ST = D / 32;                  // steps of the first product
+    constexpr int QT = Full ? 3 : 1, PT = Full ? 3 : 2;   // terms of queries, probabilities
+    constexpr int NV = 8 / C;                   // scores of a block that a lane goes on with
+    constexpr int WD = D + 2;                   // floats of a part of one head
+    constexpr int NE = 2 * kAttnWaves;          // parts in LDS
+
+    const int G = p.group, nkv = p.c.nkv, B = p.t.batch;
+    float *const part = reinterpret_cast<float *>(kl_smem);      // [NE][G][WD]
+    int *const unit = reinterpret_cast<int *>(part + NE * G * WD);   // [NE]: unit, -1: none
+    int *const ubeg = unit + NE, *const uend = ubeg + NE;        // its tiles
+    int *const wsum = uend + NE;                                 // [kAttnWaves + 1]
+    int *const last = wsum + kAttnWaves + 1;                     // [2]
+    int *const pre = last + 2;                                   // [B + 1] tiles of earlier sequences
+
+    const int tid = threadIdx.x, lane = tid & 63, k4 = lane >> 4, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int head = n % (16 / C), copy = n / (16 / C);   // of this lane's column
+    const int psl = p.c.page_log2, psm = (1 << psl) - 1;
+    const long long cap = (long long)p.t.max_pages << psl;
+
+    const auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    // the length of sequence b, -1 where it is out of range (tiles: as for 0)
+    auto checked = [&](int len) { return len < 0 || (long long)len > cap ? -1 : len; };
+    auto tiles_of = [&](int len) { return paged_tiles(max(len, 0), p.window, NK); };
+    // Tiles of the sequences up to each: one per lane of every wave, where the
+    // wave has lanes for all (no wait for the other waves: 1 us less), else in LDS.
+    const bool few = B <= 64;
+    if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
+    int len_own = 0, upto = 0, most = 0, T;
+    auto wave_scan = [&](int v) {   // inclusive sum over the lanes
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = from_lane(v, max(lane - off, 0));
+            v += lane >= off ? o : 0;
+        }
+        return v;
+    };
+    if (few) {
+        if (lane < B) len_own = checked(p.lengths[lane]);
+        const int own = lane < B ? tiles_of(len_own) : 0;
+        upto = wave_scan(own);
+        most = uni((int)wave_max((float)own));   // (exact below 2^24; above, far from any bound)
+        T = __builtin_amdgcn_readlane(upto, 63) * nkv;
+    } else {
+        if (tid == 0) pre[0] = 0;
+        int base = 0;
+        for (int b0 = 0; b0 < B; b0 += kAttnThreads) {
+            const int b = b0 + tid;
+            const int s = wave_scan(b < B ? tiles_of(checked(p.lengths[b])) : 0);
+            if (lane == 63) wsum[wave] = s;
+            __syncthreads();
+            int add = base;
+#pragma unroll
+            for (int w = 0; w < kAttnWaves; ++w) {
+                if (w < wave) add += wsum[w];
+                base += wsum[w];
+            }
+            if (b < B) pre[b + 1] = add + s;
+            __syncthreads();
+        }
+        T = uni(base) * nkv;
+    }
+    // tiles (of one KV head) of the sequences before b
+    auto before = [&](int b) {
+        if (few) return b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+        return uni(pre[b]);
+    };
+    // (through the scalar cache: a vector load would have to be waited for
+    // behind the tiles in flight)
+    auto length_at = [&](int b) {
+        if (few) return __builtin_amdgcn_readlane(len_own, b);
+        return checked(reinterpret_cast<const KL_KARG int32_t *>(
+            reinterpret_cast<uint64_t>(p.lengths))[b]);
+    };
+    // the workgroup's share [X0, X1): a unit of its own (unit_shares), or an
+    // equal share, with a workgroup for every kAttnWaves tiles
+    const int wg = blockIdx.x;
+    const bool by_unit = few && unit_shares(B * nkv, gridDim.x, most, T, kAttnWaves);
+    const Shares sh(T, by_unit ? B * nkv : min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves));
+    if (wg >= sh.np) return;
+    int X0, X1;
+    if (by_unit) {
+        const int b = uni(wg / nkv), g = wg - b * nkv, nt = before(b + 1) - before(b);
+        X0 = before(b) * nkv + g * nt;
+        X1 = X0 + nt;
+    } else {
+        X0 = uni(sh.first(wg));
+        X1 = uni(sh.first(wg + 1));
+    }
+    int x = X0 + (((X1 - X0) * wave) / kAttnWaves);
+    const int x1 = X0 + (((X1 - X0) * (wave + 1)) / kAttnWaves);
+
+    // A place in the row of tiles.
+    struct At {
+        int b, g, t, nt;     // sequence, KV head, tile of the unit, its tiles
+        int len, start;      // positions attended: [start, len); len -1: a bad length
+        int t0;              // the unit's first tile, counted from position 0
+    };
+    auto enter = [&](At &a, int b) {
+        a.b = b;
+        a.nt = before(b + 1) - before(b);
+        a.len = length_at(b);
+        a.start = paged_start(a.len, p.window);
+        a.t0 = paged_first_tile(max(a.len, 0), p.window, NK);
+    };
+    auto find = [&](int i) {
+        int lo = 0;   // before(lo) nkv <= i < before(lo + 1) nkv
+        if (few) {
+            lo = __popcll(__ballot(lane < B && upto * nkv <= i));
+        } else {
+            for (int hi = B; hi - lo > 1;) {
+                const int mid = (lo + hi) >> 1;
+                if (before(mid) * nkv <= i) lo = mid;
+                else hi = mid;
+            }
+        }
+        At a;
+        enter(a, lo);
+        const int r = i - before(lo) * nkv;
+        a.g = uni(r / a.nt);
+        a.t = r - a.g * a.nt;
+        return a;
+    };
+    auto next = [&](At a) {
+        if (++a.t == a.nt) {
+            a.t = 0;
+            if (++a.g == nkv) {
+                a.g = 0;
+                enter(a, a.b + 1);
+            }
+        }
+        return a;
+    };
+
+    // Loads.  Every tile is asked for in the same way, without branches (behind
+    // a branch around loads the compiler has to wait for all that may be in
+    // flight): positions outside the attended ones are read in the page of the
+    // nearest attended position, at their own offset, and masked when they are
+    // used; a sequence without positions reads page 0.
+    //
+    // The pages of a tile: lane i has that of the tile's i-th group of 8 positions.
+    auto ask_pages = [&](const At &a) {
+        const int pos = (a.t0 + a.t) * NK + 8 * (lane % (NK / 8));
+        const int in = max(min(max(pos, a.start), a.len - 1), 0);
+        const int page = p.t.pages[(long long)a.b * p.t.stride + (a.len > 0 ? in >> psl : 0)];
+        return page;
+    };
+    u32x4 kr[NS][2][NC];
+    unsigned vr[NS][8][VW];
+    u32x2 ksr[NS];
+    typename ScaleWord<NV>::type vsr[NS];   // of the lane's NV positions
+    typedef unsigned VWord __attribute__((ext_vector_type(VW)));
+    bool page_bad = false;   // of the tile whose keys were asked for last
+    // the row of the group of positions at 'key', whose page lane 'from' of pages has
+    auto group_row = [&](const At &a, int pages, int from, int key) {
+        return (((long long)from_lane(pages, from) * nkv + a.g) << psl) + (key & psm);
+    };
+    auto ask_keys = [&](const At &a, int &pages) {
+        if (a.len <= 0) pages = 0;
+        page_bad = __any((unsigned)pages >= (unsigned)p.c.n_pages);
+        pages = (unsigned)pages < (unsigned)p.c.n_pages ? pages : 0;
+        const int key0 = (a.t0 + a.t) * NK;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const long long r0 = group_row(a, pages, 4 * s + (n >> 2), key0 + 32 * s + 8 * (n >> 2));
+            const uint8_t *src = p.c.k + (r0 + (n & 3)) * RB + 16 * k4;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) kr[s][t][c] = ld_stream_16B(src + 4 * t * RB + 64 * c);
+            if constexpr (F8) ksr[s] = *reinterpret_cast<const u32x2 *>(p.c.ks + r0);
+        }
+    };
+    auto ask_values = [&](const At &a, int pages) {
+        const int key0 = (a.t0 + a.t) * NK;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const long long r0 = group_row(a, pages, 4 * s + k4, key0 + 32 * s + 8 * k4);
+            const uint8_t *src = p.c.v + r0 * RB + n * (EV * ES);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const VWord w = __builtin_nontemporal_load(reinterpret_cast<const VWord *>(src + j * RB));
+#pragma unroll
+                for (int i = 0; i < VW; ++i) vr[s][j][i] = w[i];
+            }
+            if constexpr (F8)
+                vsr[s] = *reinterpret_cast<const typename ScaleWord<NV>::type *>(p.c.vs + r0 + NV * copy);
+        }
+    };
+
+    // The queries of a unit as columns of the first product: asked for as they
+    // are, and taken apart into terms when they are needed.
+    constexpr int QW = Full ? 2 : 1;   // 16-byte words of 8 elements, at most
+    bf16x8 q[QT][ST];
+    auto ask_q = [&](const At &a, u32x4 (&raw)[ST][QW]) {
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            const int d0 = F8 ? 64 * (s / 2) + 16 * k4 + 8 * (s & 1) : 32 * s + 8 * k4;
+            // (columns past the group: head 0 again, masked below)
+            const long long at = a.b * p.q_row + (a.g * G + (head < G ? head : 0)) * p.q_head + d0;
+            const float *f = reinterpret_cast<const float *>(p.q) + at;
+            if (Full && p.q_type == KL_DTYPE_FP32) {
+                raw[s][0] = load_16B(f, p.q_vec);
+                raw[s][QW - 1] = load_16B(f + 4, p.q_vec);
+            } else {
+                raw[s][0] = load_16B(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
+                if (Full) raw[s][QW - 1] = raw[s][0];
+            }
+        }
+    };
+    const float sign = p.scale > 0.f ? 1.f : p.scale < 0.f ? -1.f : 0.f;
+    auto take_q = [&](const u32x4 (&raw)[ST][QW]) {
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+            if constexpr (Full) {
+                float v[8];
+                words_to_f32(raw[s][0], raw[s][QW - 1], p.q_type, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = head < G ? v[j] * sign : 0.f;
+                bf16x8 t[QT];
+                split_terms(v, t);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) q[i][s] = t[i];
+            } else {   // (bf16 queries are their own term)
+                u32x4 w = raw[s][0];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = head < G && sign != 0.f ? w[i] ^ (sign < 0.f ? 0x80008000u : 0u) : 0u;
+                q[0][s] = __builtin_bit_cast(bf16x8, w);
+            }
+        }
+    };
+
+    const int out_bytes = p.out_type == KL_DTYPE_FP32 ? 4 : 2;
+    // head h of the group, of maximum M (log2 units) and sum L
+    auto write_lse = [&](int b, int g, int h, float M, float L) {
+        p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
+    };
+    // its element dd, O unnormalised
+    auto write_out = [&](int b, int g, int h, int dd, float O, float M, float L) {
+        store1(p.out, p.out_type, b * p.out_row + (g * G + h) * p.out_head + dd, O / L);
+        if (p.lse && dd == 0) write_lse(b, g, h, M, L);
+    };
+
+    // scores are c S^T in log2 units, c > 0: a negative scale's sign is in the
+    // queries, as is a zero scale
+    const float c = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.4426950408889634f;
+    float m = -INFINITY, l = 0.f;   // the column's maximum (log2 units), this lane's share of its sum
+    f32x4 o[EV];                    // O^T: element EV (4 k4 + i) + e of head n in o[e][i]
+    auto clear = [&]() {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < EV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+
+    // the scores of the tile in kr that this lane goes on with
+    auto scores = [&](float (&s)[NS][NV]) {
+#pragma unroll
+        for (int sb = 0; sb < NS; ++sb) {
+            f32x4 st[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                float ks = 1.f;
+                if constexpr (F8) ks = pow2_of((ksr[sb][t] >> (8 * (n & 3))) & 255u);
+#pragma unroll
+                for (int e = 0; e < ST; ++e) {
+                    u32x4 w;
+                    if constexpr (F8) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const unsigned u = kr[sb][t][e / 2][2 * (e & 1) + i];
+                            w[2 * i] = fp8_to_bf16<false>(u, ks);
+                            w[2 * i + 1] = fp8_to_bf16<true>(u, ks);
+                        }
+                    } else {
+                        w = kr[sb][t][e];
+                    }
+#pragma unroll
+                    for (int i = QT - 1; i >= 0; --i)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w),
+                                                                      q[i][e], acc, 0, 0, 0);
+                }
+                st[t] = acc;
+            }
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if constexpr (C == 1) {
+                    s[sb][v] = st[v / 4][v & 3];
+                } else if constexpr (C == 2) {
+                    s[sb][v] = copy ? st[1][v] : st[0][v];
+                } else {
+                    const float lo = copy & 1 ? st[0][v + 2] : st[0][v];
+                    const float hi = copy & 1 ? st[1][v + 2] : st[1][v];
+                    s[sb][v] = copy & 2 ? hi : lo;
+                }
+            }
+        }
+    };
+    // tile a's share of m, l and o, from its scores and the values in vr
+    auto weigh = [&](const At &a, float (&s)[NS][NV]) {
+        const int key0 = (a.t0 + a.t) * NK;
+        const bool inside = key0 >= a.start && key0 + NK <= a.len;
+        if (!inside) {
+            // what is masked may hold anything: its scores, values and scales go
+#pragma unroll
+            for (int sb = 0; sb < NS; ++sb) {
+                const int k0 = key0 + 32 * sb + 8 * k4;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int key = k0 + NV * copy + v;
+                    if (key < a.start || key >= a.len) {
+                        s[sb][v] = -INFINITY;
+                        if constexpr (F8) clear_scale(vsr[sb], v);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool out = k0 + j < a.start || k0 + j >= a.len;
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) vr[sb][j][i] = out ? 0u : vr[sb][j][i];
+                }
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int sb = 0; sb < NS; ++sb)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) mx = fmaxf(mx, s[sb][v]);
+        mx *= c;
+        if (__any(mx > m + 8.f)) {
+            const float mn = fmaxf(m, over_copies<C>(max_16_32(mx), MaxOp()));
+            const float al = __builtin_amdgcn_exp2f(m - mn);
+            l *= al;
+#pragma unroll
+            for (int i = 0; i < EV; ++i) o[i] *= al;
+            m = mn;
+        }
+#pragma unroll
+        for (int sb = 0; sb < NS; ++sb) {
+            float pr[NV];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                pr[v] = __builtin_amdgcn_exp2f(fmaf(s[sb][v], c, -m));
+                l += pr[v];
+                if constexpr (F8) pr[v] *= pow2_of(scale_byte(vsr[sb], v));
+            }
+            // this lane's column has the weights of its own positions and
+            // zeros for the other copies'
+            bf16x8 pt[PT];
+#pragma unroll
+            for (int t = 0; t < PT; ++t) {
+                u32x4 w;
+                unsigned pk[NV / 2];
+#pragma unroll
+                for (int i = 0; i < NV / 2; ++i) {
+                    pk[i] = pack_bf16(pr[2 * i], pr[2 * i + 1]);
+                    if (t + 1 < PT) {
+                        pr[2 * i] -= bf_lo(pk[i]);
+                        pr[2 * i + 1] -= bf_hi(pk[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = C == 1 || copy == i / (NV / 2) ? pk[i % (NV / 2)] : 0u;
+                pt[t] = __builtin_bit_cast(bf16x8, w);
+            }
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+                constexpr int EW = F8 ? 4 : 2;   // elements per word
+                u32x4 e[EW];   // element i of the word, positions in pairs
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned v0 = vr[sb][2 * j][w], v1 = vr[sb][2 * j + 1][w];
+                    if constexpr (F8) {
+                        const unsigned u0 = __builtin_amdgcn_perm(v1, v0, 0x05010400);
+                        const unsigned u1 = __builtin_amdgcn_perm(v1, v0, 0x07030602);
+                        e[0][j] = fp8_to_bf16<false>(u0, 1.f);
+                        e[1][j] = fp8_to_bf16<true>(u0, 1.f);
+                        e[2][j] = fp8_to_bf16<false>(u1, 1.f);
+                        e[3][j] = fp8_to_bf16<true>(u1, 1.f);
+                    } else {
+                        e[0][j] = __builtin_amdgcn_perm(v1, v0, 0x05040100);
+                        e[1][j] = __builtin_amdgcn_perm(v1, v0, 0x07060302);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < EW; ++i)
+#pragma unroll
+                    for (int t = PT - 1; t >= 0; --t)
+                        o[EW * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, e[i]), pt[t], o[EW * w + i], 0, 0, 0);
+            }
+        }
+    };
+
+    if (x < x1) {
+        const int first = x;
+        clear();
+        At a = find(x);
+        // The unit of tile a ends here, or the wave's share does: a unit that is
+        // the wave's own goes out, of another the part is left in LDS.
+        bool bad = false;
+        auto flush = [&](bool ends) {
+            const int u0 = x - a.t;   // the unit's first tile, in the row of all
+            if (bad) {
+                l = __builtin_nanf("");
+                if (lane == 0) flag_error(p.error, a.len < 0 ? KL_DEVERR_POSITION : KL_DEVERR_PAGE);
+            }
+            float L = over_copies<C>(sum_16_32(l), AddOp());
+            if constexpr (C > 1) {
+#pragma unroll
+                for (int e = 0; e < EV; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[e][i] = over_copies<C>(o[e][i], AddOp());
+            }
+            if (a.len == 0) {   // (nothing attended: what was computed is void)
+                clear();
+                L = 1.f;
+            }
+            // into LDS: a unit's part, or a whole unit on its way out (in the
+            // place of the part that the wave may end with)
+            const bool whole = ends && u0 >= first;
+            const int slot = 2 * wave + (u0 >= first);
+            float *const w = part + slot * G * WD;
+            if (n < G) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < EV; ++e) w[n * WD + EV * (4 * k4 + i) + e] = o[e][i];
+                if (k4 == 0) {
+                    w[n * WD + D] = m;
+                    w[n * WD + D + 1] = L;
+                }
+            }
+            if (whole) {
+                __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses are in order)
+                for (int i = 8 * lane; i < G * D; i += 512) {
+                    const int h = i / D, dd = i % D;
+                    const float *const r = w + h * WD;
+                    const float inv = 1.f / r[D + 1];
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = r[dd + j] * inv;
+                    store8(reinterpret_cast<uint8_t *>(p.out) +
+                               (a.b * p.out_row + (a.g * G + h) * p.out_head + dd) * out_bytes,
+                           p.out_type, p.out_vec, v);
+                    if (p.lse && dd == 0) write_lse(a.b, a.g, h, r[D], r[D + 1]);
+                }
+                __builtin_amdgcn_wave_barrier();
+            } else if (lane == 0) {
+                unit[slot] = a.b * nkv + a.g;
+                ubeg[slot] = u0;
+                uend[slot] = u0 + a.nt;
+            }
+        };
+        int pg = ask_pages(a);
+        At an = a;
+        if (x + 1 < x1) an = next(a);
+        int pgn = ask_pages(an);
+        {
+            u32x4 raw[ST][QW];
+            ask_q(a, raw);
+            ask_keys(a, pg);
+            // (values behind keys, here as in the loop: what waits for keys then
+            // need not wait for values)
+            __builtin_amdgcn_sched_barrier(0);
+            ask_values(a, pg);
+            take_q(raw);
+        }
+        bad = a.len < 0 || page_bad;
+        // While a tile is worked on the next one's loads run: its keys are asked
+        // for once this one's are used, its values likewise, its pages a tile
+        // earlier.
+        for (; x + 1 < x1; ++x) {
+            float s[NS][NV];
+            scores(s);
+            ask_keys(an, pgn);
+            At ann = an;
+            if (x + 2 < x1) ann = next(an);
+            const int pgnn = ask_pages(ann);
+            weigh(a, s);
+            ask_values(an, pgn);
+            if (a.t + 1 == a.nt) {
+                flush(true);
+                clear();
+                bad = false;
+                u32x4 raw[ST][QW];
+                ask_q(an, raw);
+                take_q(raw);
+                // (nothing in flight on either way out of this branch that the
+                // other does not know of)
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+            }
+            bad = bad || an.len < 0 || page_bad;
+            a = an;
+            an = ann;
+            pg = pgn;
+            pgn = pgnn;
+        }
+        float s[NS][NV];
+        scores(s);
+        weigh(a, s);
+        flush(a.t + 1 == a.nt);
+    }
+    __syncthreads();
+
+    // join the parts in LDS, run by run of one unit's (lane i: part i)
+    // units handed on and their workgroups: one that began earlier, one that goes on
+    int sent0 = -1, sent1 = -1, count0 = 0, count1 = 0;
+    const int own_unit = lane < NE ? unit[lane] : -1;
+    unsigned left = (unsigned)__ballot(own_unit >= 0);
+    while (left) {
+        const int e = __builtin_ctz(left);
+        const int u = __builtin_amdgcn_readlane(own_unit, e);
+        const unsigned run = (unsigned)__ballot(own_unit == u);
+        left &= ~run;
+        const int b0 = __builtin_amdgcn_readfirstlane(ubeg[e]);
+        const int b1 = __builtin_amdgcn_readfirstlane(uend[e]);
+        const bool whole = b0 >= X0 && b1 <= X1;
+        const int z = b0 >= X0;
+        if (!whole) {
+            const int nw = sh.of(b1 - 1) - sh.of(b0) + 1;
+            if (z) sent1 = u, count1 = nw;
+            else sent0 = u, count0 = nw;
+        }
+        for (int i = tid; i < G * D; i += kAttnThreads) {
+            const int h = i / D, dd = i % D;
+            constexpr int NB = 8;   // parts read together (a run has 9 at most)
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            for (unsigned r = run; r;) {
+                int k[NB], nk = 0;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    k[j] = r ? __builtin_ctz(r) : e;
+                    nk += r != 0;
+                    r &= r - 1;
+                }
+                join_parts<NB>(nk, O, M, L, [&](int j, float &o, float &m, float &l) {
+                    const float *w = part + (k[j] * G + h) * WD;
+                    m = w[D];
+                    l = w[D + 1];
+                    o = w[dd];
+                });
+            }
+            if (whole) {
+                write_out(u / nkv, u % nkv, h, dd, O, M, L);
+            } else {
+                float *w = p.parts + ((size_t)(wg * 2 + z) * G + h) * WD;
+                st_dev(w + dd, O);
+                if (dd == 0) {
+                    st_dev(w + D, M);
+                    st_dev(w + D + 1, L);
+                }
+            }
+        }
+    }
+    if (sent0 < 0 && sent1 < 0) return;
+
+    // arrive with what was handed on; the last to arrive joins a unit's parts
+    wait_stores();
+    __syncthreads();
+    if (tid < 2) {
+        const int u = tid ? sent1 : sent0, nw = tid ? count1 : count0;
+        int mine = 0;
+        if (u >= 0)
+            mine = __hip_atomic_fetch_add(p.arrived + u, 1u, __ATOMIC_RELAXED,
+                                          __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(nw - 1);
+        if (mine)
+            __hip_atomic_store(p.arrived + u, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last[tid] = mine;
+    }
+    __syncthreads();
+    for (int z = 0; z < 2; ++z) {
+        if (!__builtin_amdgcn_readfirstlane(last[z])) continue;
+        const int u = z ? sent1 : sent0, nw = z ? count1 : count0;
+        const int b = u / nkv, g = u % nkv;
+        const int f = sh.of(before(b) * nkv + g * (before(b + 1) - before(b)));
+        for (int i = tid; i < G * D; i += kAttnThreads) {
+            const int h = i / D, dd = i % D;
+            constexpr int NB = 16;   // parts whose loads are issued together
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            for (int k0 = 0; k0 < nw; k0 += NB)
+                join_parts<NB>(nw - k0, O, M, L, [&](int j, float &o, float &m, float &l) {
+                    const int k = min(k0 + j, nw - 1);
+                    const float *w = p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
+                    m = ld_dev(w + D);
+                    l = ld_dev(w + D + 1);
+                    o = ld_dev(w + dd);
+                });
+            write_out(b, g, h, dd, O, M, L);
+        }
+    }
+}
+
+template <int D, bool F8, bool Full, int C>
+static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
+    const auto kernel = kl_paged_attention_kernel<D, F8, Full, C>;
+    const int lds = 4 * (2 * kAttnWaves * (p.group * (D + 2) + 3) + kAttnWaves + 3 + p.t.batch + 1);
+    // (more than the default 64 KiB: once per device)
+    if (lds > 65536) {
+        static std::atomic<unsigned long long> done{0};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        const unsigned long long bit = 1ull << (dev & 63);
+        if (!(done.load(std::memory_order_relaxed) & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLdsMost);
+            if (e != hipSuccess) return e;
+            done.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    // at most a workgroup for every kAttnWaves tiles that the table has room for
+    const long long tiles = (((long long)p.t.max_pages << p.c.page_log2) + paged_tile(D, F8 ? 1 : 2) - 1) /
+                            paged_tile(D, F8 ? 1 : 2) * p.t.batch * p.c.nkv;
+    // (or for every unit)
+    const int grid = (int)std::min<long long>(
+        std::max<long long>((tiles + kAttnWaves - 1) / kAttnWaves, (long long)p.t.batch * p.c.nkv),
+        kPagedGroups);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kAttnThreads), lds, stream, p);
+    return hipGetLastError();
+}
+
+// The instance for the pool's type, the terms and the group's copies.
+template <int D, bool F8, bool Full>
+static hipError_t launch_copies(const AttnParams &p, hipStream_t stream) {
+    if (p.group <= 4) return launch_attention<D, F8, Full, 4>(p, stream);
+    if (p.group <= 8) return launch_attention<D, F8, Full, 2>(p, stream);
+    return launch_attention<D, F8, Full, 1>(p, stream);
+}
+template <int D>
+static hipError_t launch_attention_for(const AttnParams &p, hipStream_t stream) {
+    const bool full = p.q_type != KL_DTYPE_BF16 || p.out_type == KL_DTYPE_FP32;
+    if (p.c.e4m3) return full ? launch_copies<D, true, true>(p, stream) : launch_copies<D, true, false>(p, stream);
+    return full ? launch_copies<D, false, true>(p, stream) : launch_copies<D, false, false>(p, stream);
+}
+
+}  // namespace kl

@@ -273,16 +273,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 
     // Loads.  Every tile is asked for in the same way, without branches (behind
     // a branch around loads the compiler has to wait for all that may be in
-    // flight): positions outside the attended ones are read in the page of the
-    // nearest attended position, at their own offset, and masked when they are
-    // used; a sequence without positions reads page 0.
+    // flight): a group of 8 positions without an attended one reads the nearest
+    // group that has one, a sequence without positions page 0, and what is not
+    // attended is masked when it is used.
     //
     // The pages of a tile: lane i has that of the tile's i-th group of 8 positions.
+    auto nearest = [&](const At &a, int pos) { return max(min(max(pos, a.start), a.len - 1), 0); };
     auto ask_pages = [&](const At &a) {
-        const int pos = (a.t0 + a.t) * NK + 8 * (lane % (NK / 8));
-        const int in = max(min(max(pos, a.start), a.len - 1), 0);
-        const int page = p.t.pages[(long long)a.b * p.t.stride + (a.len > 0 ? in >> psl : 0)];
-        return page;
+        const int pos = nearest(a, (a.t0 + a.t) * NK + 8 * (lane % (NK / 8)));
+        return p.t.pages[(long long)a.b * p.t.stride + (pos >> psl)];
     };
     u32x4 kr[NS][2][NC];
     unsigned vr[NS][8][VW];
@@ -290,9 +289,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     typename ScaleWord<NV>::type vsr[NS];   // of the lane's NV positions
     typedef unsigned VWord __attribute__((ext_vector_type(VW)));
     bool page_bad = false;   // of the tile whose keys were asked for last
-    // the row of the group of positions at 'key', whose page lane 'from' of pages has
+    // the first row of the group of positions at 'key', whose page lane 'from' of pages has
     auto group_row = [&](const At &a, int pages, int from, int key) {
-        return (((long long)from_lane(pages, from) * nkv + a.g) << psl) + (key & psm);
+        return (((long long)from_lane(pages, from) * nkv + a.g) << psl) +
+               (nearest(a, key) & psm & ~7);
     };
     auto ask_keys = [&](const At &a, int &pages) {
         if (a.len <= 0) pages = 0;
@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         // The unit of tile a ends here, or the wave's share does: a unit that is
         // the wave's own goes out, of another the part is left in LDS.
         bool bad = false;
-        auto flush = [&](bool ends) {
+        auto flush = [&](bool ends, auto &&between) {
             const int u0 = x - a.t;   // the unit's first tile, in the row of all
             if (bad) {
                 l = __builtin_nanf("");
@@ -573,6 +573,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                     w[n * WD + D + 1] = L;
                 }
             }
+            between();
             if (whole) {
                 __builtin_amdgcn_wave_barrier();   // (a wave's LDS accesses are in order)
                 for (int i = 8 * lane; i < G * D; i += 512) {
@@ -622,15 +623,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             weigh(a, s);
             ask_values(an, pgn);
             if (a.t + 1 == a.nt) {
-                flush(true);
-                clear();
-                bad = false;
                 u32x4 raw[ST][QW];
                 ask_q(an, raw);
-                take_q(raw);
-                // (nothing in flight on either way out of this branch that the
-                // other does not know of)
-                __builtin_amdgcn_s_waitcnt(0x0F70);
+                // (taken before the results are stored: no later wait for loads
+                // then waits for stores)
+                flush(true, [&]() { take_q(raw); });
+                clear();
+                bad = false;
             }
             bad = bad || an.len < 0 || page_bad;
             a = an;
@@ -641,7 +640,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         float s[NS][NV];
         scores(s);
         weigh(a, s);
-        flush(a.t + 1 == a.nt);
+        flush(a.t + 1 == a.nt, []() {});
     }
     __syncthreads();
 

@@ -10,9 +10,10 @@ namespace kl {
 // Rows.  A group of lanes, 8 for head_dim 64 and 16 for 128 (8 elements each),
 // has R rows of the call, of one head and of K or V.  Its first R lanes look up
 // a row's slot each; all R rows are in flight together, and their scale bytes
-// move in one access, a byte per lane.  Both kernels are bound by HBM: at the
-// largest sizes R = 8 (32768 rows of 8 heads of 128, bf16 to e4m3: 66 us with
-// R = 1), where the rows do not fill the chip, R = 1 (row_params below).
+// move in one access, a byte per lane.  Both kernels are bound by HBM (32768
+// rows of 8 heads of 128, bf16 to e4m3: 47 us, 4.3 TB/s; 24402 rows e4m3 to fp32:
+// 40 us, 6.3 TB/s; with R = 1 66 and 73, with R = 8 51 and 42).  How many rows a
+// group takes: many_rows below.
 
 // The pool row of (row r of the call, head): its index among the layer's rows
 // of heads, -1 for a padding row (or none), -2 for a bad one.
@@ -113,7 +114,9 @@ __global__ void __launch_bounds__(256) kl_paged_append_kernel(RowParams p) {
                 w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, w[k], true);
             }
             if (bad) w[0] = w[1] = 0x7f7f7f7f;   // (NaN)
-            if (row >= 0) *reinterpret_cast<int2 *>(pool + row * D + 8 * j) = make_int2(w[0], w[1]);
+            if (row >= 0) 
+                __builtin_nontemporal_store(u32x2{(unsigned)w[0], (unsigned)w[1]},
+                                            reinterpret_cast<u32x2 *>(pool + row * D + 8 * j));
             if (j == i) scale = bad ? 127 : e + 127;
         }
         if (p.c.e4m3 && own >= 0) (m.is_v ? p.c.vs : p.c.ks)[own] = (uint8_t)scale;
@@ -179,8 +182,8 @@ __global__ void __launch_bounds__(256) kl_paged_read_kernel(RowParams p) {
             if constexpr (Wide) {
                 float *o0 = reinterpret_cast<float *>(out) + e0, *o1 = reinterpret_cast<float *>(out) + e1;
                 if (vec) {
-                    *reinterpret_cast<f32x4 *>(o0) = f32x4{x[0], x[1], x[2], x[3]};
-                    *reinterpret_cast<f32x4 *>(o1) = f32x4{x[4], x[5], x[6], x[7]};
+                    store_16B(o0, f32x4{x[0], x[1], x[2], x[3]});
+                    store_16B(o1, f32x4{x[4], x[5], x[6], x[7]});
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o0[k] = x[k], o1[k] = x[4 + k];
@@ -192,10 +195,10 @@ __global__ void __launch_bounds__(256) kl_paged_read_kernel(RowParams p) {
     }
 }
 
-// Rows that a group takes: 8 where the groups then still fill the chip twice
-// over (256 compute units of 8 waves), else 1.
+// A group takes 4 rows where the groups then still make 8 waves for each of 256
+// compute units, else one.
 static bool many_rows(const RowParams &p) {
-    return (p.rows / 8 * 2 * p.c.nkv) * (p.c.d / 8) >= 2 * 256 * 8 * 64;
+    return (p.rows / 4 * 2 * p.c.nkv) * (p.c.d / 8) >= 256 * 8 * 64;
 }
 template <class Kernel>
 static hipError_t launch_rows(Kernel kernel, const RowParams &p, int R, hipStream_t stream) {
@@ -207,12 +210,12 @@ static hipError_t launch_rows(Kernel kernel, const RowParams &p, int R, hipStrea
 
 template <int D>
 static hipError_t append_for(const RowParams &p, hipStream_t stream) {
-    return many_rows(p) ? launch_rows(kl_paged_append_kernel<D, 8>, p, 8, stream)
+    return many_rows(p) ? launch_rows(kl_paged_append_kernel<D, 4>, p, 4, stream)
                         : launch_rows(kl_paged_append_kernel<D, 1>, p, 1, stream);
 }
 template <int D, bool Wide>
 static hipError_t read_for(const RowParams &p, hipStream_t stream) {
-    return many_rows(p) ? launch_rows(kl_paged_read_kernel<D, 8, Wide>, p, 8, stream)
+    return many_rows(p) ? launch_rows(kl_paged_read_kernel<D, 4, Wide>, p, 4, stream)
                         : launch_rows(kl_paged_read_kernel<D, 1, Wide>, p, 1, stream);
 }
 

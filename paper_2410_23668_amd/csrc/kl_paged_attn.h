@@ -339,10 +339,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             const long long at = a.b * p.q_row + (a.g * G + (head < G ? head : 0)) * p.q_head + d0;
             const float *f = reinterpret_cast<const float *>(p.q) + at;
             if (Full && p.q_type == KL_DTYPE_FP32) {
-                raw[s][0] = load_16B(f, p.q_vec);
-                raw[s][QW - 1] = load_16B(f + 4, p.q_vec);
+                raw[s][0] = load_16B<false>(f, p.q_vec);
+                raw[s][QW - 1] = load_16B<false>(f + 4, p.q_vec);
             } else {
-                raw[s][0] = load_16B(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
+                raw[s][0] = load_16B<false>(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
                 if (Full) raw[s][QW - 1] = raw[s][0];
             }
         }

@@ -197,16 +197,22 @@ class PagedKvCache:
             self.device.index)
 
     def _table(self, table: torch.Tensor) -> kb.kl_page_table:
-        assert table.dtype == torch.int32 and table.dim() == 2 and table.device == self.device
-        assert table.shape[1] <= 1 or table.stride(1) == 1
-        batch, n = table.shape
-        return kb.kl_page_table(table.data_ptr(), batch, n,
-                                table.stride(0) if batch > 1 else n)
+        (batch, n), (row, one) = table.shape, table.stride()
+        assert table.dtype == torch.int32 and table.device == self.device
+        assert one == 1 or n <= 1
+        return kb.kl_page_table(table.data_ptr(), batch, n, row if batch > 1 else n)
 
     def _rows(self, x: torch.Tensor, rows: int, heads: int) -> kb.kl_rows:
-        assert x.shape == (rows, heads, self.head_dim) and x.stride(2) == 1
-        assert x.device == self.device
-        return kb.kl_rows(x.data_ptr(), _DTYPES[x.dtype], x.stride(0), x.stride(1))
+        row, head, one = x.stride()
+        assert x.shape == (rows, heads, self.head_dim) and one == 1 and x.device == self.device
+        assert x.dtype in _DTYPES
+        return kb.kl_rows(x.data_ptr(), _DTYPES[x.dtype], row, head)
+
+    def _stream(self, stream: torch.cuda.Stream | None) -> int:
+        if stream is not None:
+            return stream.cuda_stream
+        # (the current stream without a Stream object, which takes 2.6 us to make)
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def _slots(self, positions, seq) -> tuple:
         assert positions.dtype == torch.int32 and positions.dim() == 1
@@ -224,7 +230,7 @@ class PagedKvCache:
         s, p, n = self._slots(positions, seq)
         kb.kl_paged_append(self.c, layer, self._table(table), s, p, n,
                            self._rows(k, n, self.n_kv), self._rows(v, n, self.n_kv),
-                           self.error.data_ptr(), stream_handle(stream))
+                           self.error.data_ptr(), self._stream(stream))
 
     def read(self, layer: int, table: torch.Tensor, positions: torch.Tensor, k: torch.Tensor,
              v: torch.Tensor, seq: torch.Tensor | None = None,
@@ -233,7 +239,7 @@ class PagedKvCache:
         s, p, n = self._slots(positions, seq)
         kb.kl_paged_read(self.c, layer, self._table(table), s, p, n,
                          self._rows(k, n, self.n_kv), self._rows(v, n, self.n_kv),
-                         self.error.data_ptr(), stream_handle(stream))
+                         self.error.data_ptr(), self._stream(stream))
 
     def workspace(self, batch: int) -> torch.Tensor:
         """A workspace for attention calls of up to 'batch' sequences, one after
@@ -263,7 +269,7 @@ class PagedKvCache:
                               self.head_dim ** -0.5 if scale is None else scale, window,
                               self._rows(out, B, heads),
                               lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
-                              workspace.numel(), self.error.data_ptr(), stream_handle(stream))
+                              workspace.numel(), self.error.data_ptr(), self._stream(stream))
 
     def device_error(self) -> int:
         """Synchronizes; the error bits of this pool's calls so far, which are then cleared."""

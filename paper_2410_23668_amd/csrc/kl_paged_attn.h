@@ -80,25 +80,31 @@ __device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
     }
 }
 
-// Adds the first n (at most NB) of the parts that get(j, output, maximum, sum)
-// reads, all of them at once, to (O, M, L).
+// Two neighbouring outputs of a head, unnormalised, with their maximum (log2
+// units) and sum.
+struct Joined { float o0 = 0.f, o1 = 0.f, m = -INFINITY, l = 0.f; };
+// Adds the first n (at most NB) of the parts that get(j, outputs, (maximum,
+// sum)) reads, all of them at once.
 template <int NB, class Get>
-__device__ __forceinline__ void join_parts(int n, float &O, float &M, float &L, Get &&get) {
-    float o[NB], m[NB], l[NB], mn = M;
+__device__ __forceinline__ void join_parts(int n, Joined &a, Get &&get) {
+    f32x2 o[NB], ml[NB];
+    float mn = a.m;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) get(j, o[j], m[j], l[j]);
+    for (int j = 0; j < NB; ++j) get(j, o[j], ml[j]);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) mn = j < n ? fmaxf(mn, m[j]) : mn;
-    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);   // (none yet: 0)
-    L *= a;
-    O *= a;
+    for (int j = 0; j < NB; ++j) mn = j < n ? fmaxf(mn, ml[j][0]) : mn;
+    const float al = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - mn);   // (none yet: 0)
+    a.l *= al;
+    a.o0 *= al;
+    a.o1 *= al;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        const float w = __builtin_amdgcn_exp2f(m[j] - mn);
-        L = j < n ? fmaf(l[j], w, L) : L;
-        O = j < n ? fmaf(o[j], w, O) : O;
+        const float w = __builtin_amdgcn_exp2f(ml[j][0] - mn);
+        a.l = j < n ? fmaf(ml[j][1], w, a.l) : a.l;
+        a.o0 = j < n ? fmaf(o[j][0], w, a.o0) : a.o0;
+        a.o1 = j < n ? fmaf(o[j][1], w, a.o1) : a.o1;
     }
-    M = mn;
+    a.m = mn;
 }
 
 // Scale bytes of N consecutive positions, and the i-th.
@@ -130,6 +136,12 @@ __device__ __forceinline__ float over_copies(float v, Op op) {
     return v;
 }
 
+// Floats of LDS for the waves' parts (and, at the end, for four floats a thread).
+__host__ __device__ constexpr int attn_part_floats(int group, int d) {
+    return 2 * kAttnWaves * group * (d + 2) > 4 * kAttnThreads ? 2 * kAttnWaves * group * (d + 2)
+                                                               : 4 * kAttnThreads;
+}
+
 template <int D, bool F8, bool Full, int C>
 __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(AttnParams p) {
     constexpr int ES = F8 ? 1 : 2;
@@ -145,10 +157,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 
     const int G = p.group, nkv = p.c.nkv, B = p.t.batch;
     float *const part = reinterpret_cast<float *>(kl_smem);      // [NE][G][WD]
-    int *const unit = reinterpret_cast<int *>(part + NE * G * WD);   // [NE]: unit, -1: none
-    int *const ubeg = unit + NE, *const uend = ubeg + NE;        // its tiles
-    int *const wsum = uend + NE;                                 // [kAttnWaves + 1]
-    int *const last = wsum + kAttnWaves + 1;                     // [2]
+    int *const unit = reinterpret_cast<int *>(part + attn_part_floats(G, D));   // [NE]: unit, -1: none
+    int *const wsum = unit + NE;                                 // [kAttnWaves]
+    int *const last = wsum + kAttnWaves;                         // [2]
     int *const pre = last + 2;                                   // [B + 1] tiles of earlier sequences
 
     const int tid = threadIdx.x, lane = tid & 63, k4 = lane >> 4, n = lane & 15;
@@ -166,9 +177,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     const bool few = B <= 64;
     if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
     int len_own = 0, upto = 0, most = 0, T;
-    auto wave_scan = [&](int v) {   // inclusive sum over the lanes
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
+    auto wave_scan = [&](int v) {   // inclusive sum over the lanes (zero past B)
+        for (int off = 1; off < 64 && off < B; off <<= 1) {
             const int o = from_lane(v, max(lane - off, 0));
             v += lane >= off ? o : 0;
         }
@@ -179,7 +189,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         const int own = lane < B ? tiles_of(len_own) : 0;
         upto = wave_scan(own);
         most = uni((int)wave_max((float)own));   // (exact below 2^24; above, far from any bound)
-        T = __builtin_amdgcn_readlane(upto, 63) * nkv;
+        T = __builtin_amdgcn_readlane(upto, B - 1) * nkv;
     } else {
         if (tid == 0) pre[0] = 0;
         int base = 0;
@@ -375,10 +385,20 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     auto write_lse = [&](int b, int g, int h, float M, float L) {
         p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
     };
-    // its element dd, O unnormalised
-    auto write_out = [&](int b, int g, int h, int dd, float O, float M, float L) {
-        store1(p.out, p.out_type, b * p.out_row + (g * G + h) * p.out_head + dd, O / L);
-        if (p.lse && dd == 0) write_lse(b, g, h, M, L);
+    // its elements dd and dd + 1
+    auto write_pair = [&](int b, int g, int h, int dd, const Joined &a) {
+        const long long at = b * p.out_row + (g * G + h) * p.out_head + dd;
+        const float inv = 1.f / a.l, x0 = a.o0 * inv, x1 = a.o1 * inv;
+        if (p.out_type == KL_DTYPE_FP32 && p.out_vec) {
+            *reinterpret_cast<f32x2 *>(reinterpret_cast<float *>(p.out) + at) = f32x2{x0, x1};
+        } else if (p.out_vec) {
+            *reinterpret_cast<unsigned *>(reinterpret_cast<uint16_t *>(p.out) + at) =
+                bits16(x0, p.out_type) | ((unsigned)bits16(x1, p.out_type) << 16);
+        } else {
+            store1(p.out, p.out_type, at, x0);
+            store1(p.out, p.out_type, at + 1, x1);
+        }
+        if (p.lse && dd == 0) write_lse(b, g, h, a.m, a.l);
     };
 
     // scores are c S^T in log2 units, c > 0: a negative scale's sign is in the
@@ -534,6 +554,25 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         }
     };
 
+    // Units of several workgroups: the one that the share begins inside of, and
+    // the one that begins in the share and goes on behind it; each one's first
+    // workgroup and their number.
+    int sent0 = -1, sent1 = -1, from0 = 0, count0 = 0, count1 = 0;
+    auto find_shared = [&]() {
+        if (by_unit) return;
+        const At h = find(X0), e = find(X1 - 1);
+        const int hb = X0 - h.t, eb = X1 - 1 - e.t;
+        if (h.t > 0) {
+            sent0 = h.b * nkv + h.g;
+            from0 = uni(sh.of(hb));
+            count0 = uni(sh.of(hb + h.nt - 1)) - from0 + 1;
+        }
+        if (eb >= X0 && eb + e.nt > X1) {
+            sent1 = e.b * nkv + e.g;
+            count1 = uni(sh.of(eb + e.nt - 1)) - wg + 1;
+        }
+    };
+
     if (x < x1) {
         const int first = x;
         clear();
@@ -591,8 +630,6 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 __builtin_amdgcn_wave_barrier();
             } else if (lane == 0) {
                 unit[slot] = a.b * nkv + a.g;
-                ubeg[slot] = u0;
-                uend[slot] = u0 + a.nt;
             }
         };
         int pg = ask_pages(a);
@@ -607,6 +644,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             // need not wait for values)
             __builtin_amdgcn_sched_barrier(0);
             ask_values(a, pg);
+            find_shared();   // (while the loads run)
             take_q(raw);
         }
         bad = a.len < 0 || page_bad;
@@ -641,12 +679,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         scores(s);
         weigh(a, s);
         flush(a.t + 1 == a.nt, []() {});
+    } else {
+        find_shared();
     }
     __syncthreads();
 
-    // join the parts in LDS, run by run of one unit's (lane i: part i)
-    // units handed on and their workgroups: one that began earlier, one that goes on
-    int sent0 = -1, sent1 = -1, count0 = 0, count1 = 0;
+    // join the parts in LDS, run by run of one unit's (lane i: part i), a pair of
+    // outputs per thread
+    const int pairs = G * D / 2;
     const int own_unit = lane < NE ? unit[lane] : -1;
     unsigned left = (unsigned)__ballot(own_unit >= 0);
     while (left) {
@@ -654,43 +694,25 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         const int u = __builtin_amdgcn_readlane(own_unit, e);
         const unsigned run = (unsigned)__ballot(own_unit == u);
         left &= ~run;
-        const int b0 = __builtin_amdgcn_readfirstlane(ubeg[e]);
-        const int b1 = __builtin_amdgcn_readfirstlane(uend[e]);
-        const bool whole = b0 >= X0 && b1 <= X1;
-        const int z = b0 >= X0;
-        if (!whole) {
-            const int nw = sh.of(b1 - 1) - sh.of(b0) + 1;
-            if (z) sent1 = u, count1 = nw;
-            else sent0 = u, count0 = nw;
-        }
-        for (int i = tid; i < G * D; i += kAttnThreads) {
-            const int h = i / D, dd = i % D;
-            constexpr int NB = 8;   // parts read together (a run has 9 at most)
-            float M = -INFINITY, L = 0.f, O = 0.f;
-            for (unsigned r = run; r;) {
-                int k[NB], nk = 0;
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    k[j] = r ? __builtin_ctz(r) : e;
-                    nk += r != 0;
-                    r &= r - 1;
-                }
-                join_parts<NB>(nk, O, M, L, [&](int j, float &o, float &m, float &l) {
-                    const float *w = part + (k[j] * G + h) * WD;
-                    m = w[D];
-                    l = w[D + 1];
-                    o = w[dd];
-                });
-            }
+        const bool whole = u != sent0 && u != sent1;
+        const int nr = __builtin_popcount(run);
+        for (int i = tid; i < pairs; i += kAttnThreads) {
+            const int h = i / (D / 2), dd = 2 * (i % (D / 2));
+            Joined a;
+            // (each wave has one part of a unit at most)
+            unsigned r = run;
+            join_parts<kAttnWaves>(nr, a, [&](int, f32x2 &o, f32x2 &ml) {
+                const float *w = part + ((r ? __builtin_ctz(r) : e) * G + h) * WD;
+                r &= r - 1;
+                o = *reinterpret_cast<const f32x2 *>(w + dd);
+                ml = *reinterpret_cast<const f32x2 *>(w + D);
+            });
             if (whole) {
-                write_out(u / nkv, u % nkv, h, dd, O, M, L);
+                write_pair(u / nkv, u % nkv, h, dd, a);
             } else {
-                float *w = p.parts + ((size_t)(wg * 2 + z) * G + h) * WD;
-                st_dev(w + dd, O);
-                if (dd == 0) {
-                    st_dev(w + D, M);
-                    st_dev(w + D + 1, L);
-                }
+                float *w = p.parts + ((size_t)(wg * 2 + (u == sent1)) * G + h) * WD;
+                st_dev_f2(w + dd, a.o0, a.o1);
+                if (dd == 0) st_dev_f2(w + D, a.m, a.l);
             }
         }
     }
@@ -710,24 +732,43 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         last[tid] = mine;
     }
     __syncthreads();
+    constexpr int NB = 16;   // parts whose loads are issued together
     for (int z = 0; z < 2; ++z) {
-        if (!__builtin_amdgcn_readfirstlane(last[z])) continue;
-        const int u = z ? sent1 : sent0, nw = z ? count1 : count0;
-        const int b = u / nkv, g = u % nkv;
-        const int f = sh.of(before(b) * nkv + g * (before(b + 1) - before(b)));
-        for (int i = tid; i < G * D; i += kAttnThreads) {
-            const int h = i / D, dd = i % D;
-            constexpr int NB = 16;   // parts whose loads are issued together
-            float M = -INFINITY, L = 0.f, O = 0.f;
-            for (int k0 = 0; k0 < nw; k0 += NB)
-                join_parts<NB>(nw - k0, O, M, L, [&](int j, float &o, float &m, float &l) {
-                    const int k = min(k0 + j, nw - 1);
-                    const float *w = p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
-                    m = ld_dev(w + D);
-                    l = ld_dev(w + D + 1);
-                    o = ld_dev(w + dd);
-                });
-            write_out(b, g, h, dd, O, M, L);
+        if (!uni(last[z])) continue;
+        const int u = z ? sent1 : sent0, nw = z ? count1 : count0, f = z ? wg : from0;
+        // (where there are more parts, and a group's pairs leave threads over,
+        // S times as many threads take every S-th part: a round trip less, for
+        // an exchange in LDS)
+        const int S = nw > NB ? max(1, min(uni(kAttnThreads / pairs), (nw + NB - 1) / NB)) : 1;
+        const int sub = S > 1 ? tid / pairs : 0;
+        for (int i0 = 0; i0 < pairs; i0 += kAttnThreads) {
+            const int i = S > 1 ? tid - sub * pairs : i0 + tid;
+            const int h = i / (D / 2), dd = 2 * (i % (D / 2));
+            Joined a;
+            if (sub < S && i < pairs) {
+                for (int k0 = sub; k0 < nw; k0 += S * NB)
+                    join_parts<NB>((nw - k0 + S - 1) / S, a, [&](int j, f32x2 &o, f32x2 &ml) {
+                        const int k = min(k0 + j * S, nw - 1);
+                        const float *w = p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
+                        o = ld_dev_f2(w + dd);
+                        ml = ld_dev_f2(w + D);
+                    });
+            }
+            if (S > 1) {
+                f32x4 *const x = reinterpret_cast<f32x4 *>(part);
+                x[tid] = f32x4{a.o0, a.o1, a.m, a.l};
+                __syncthreads();
+                if (sub == 0) {
+                    for (int k = 1; k < min(S, nw); ++k)
+                        join_parts<1>(1, a, [&](int, f32x2 &o, f32x2 &ml) {
+                            const f32x4 v = x[tid + k * pairs];
+                            o = f32x2{v[0], v[1]};
+                            ml = f32x2{v[2], v[3]};
+                        });
+                }
+                __syncthreads();
+            }
+            if (sub == 0 && i < pairs) write_pair(u / nkv, u % nkv, h, dd, a);
         }
     }
 }
@@ -735,7 +776,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 template <int D, bool F8, bool Full, int C>
 static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
     const auto kernel = kl_paged_attention_kernel<D, F8, Full, C>;
-    const int lds = 4 * (2 * kAttnWaves * (p.group * (D + 2) + 3) + kAttnWaves + 3 + p.t.batch + 1);
+    const int lds = 4 * (attn_part_floats(p.group, D) + 2 * kAttnWaves + kAttnWaves + 2 + p.t.batch + 1);
     // (more than the default 64 KiB: once per device)
     if (lds > 65536) {
         static std::atomic<unsigned long long> done{0};

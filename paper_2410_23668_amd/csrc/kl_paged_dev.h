@@ -102,4 +102,14 @@ __device__ __forceinline__ void store8(void *p, int type, bool vec, const float 
     }
 }
 
+// Two floats written and read as one device-coherent word (8-byte aligned).
+__device__ __forceinline__ void st_dev_f2(float *p, float a, float b) {
+    st_dev_u64(reinterpret_cast<unsigned long long *>(p),
+               (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a));
+}
+__device__ __forceinline__ f32x2 ld_dev_f2(const float *p) {
+    const unsigned long long v = ld_dev_u64(p);
+    return f32x2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
+}
+
 }  // namespace kl

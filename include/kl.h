@@ -359,6 +359,26 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
                              float *lse, void *workspace, size_t workspace_bytes, int32_t *error,
                              void *stream);
 
+/* kl_decode_step over a paged cache: sequence b's row of the page table says
+ * where its positions are; the step writes the new token's K/V to position
+ * positions[b]'s slot of every layer (as kl_paged_append) and attends over
+ * positions 0..positions[b] (as kl_paged_attention), so an e4m3 pool halves
+ * the cache that a step reads.  It runs on the matrix-core path at every batch,
+ * one launch per operator group with the two operators in place of the
+ * attention's (6 L + 3 dispatches).
+ *   cache    of the model's n_layers, n_kv_heads, head_dim and device
+ *   table    batch >= the step's; positions are < max_pages * page_size and
+ *            < max_seq
+ * The other arguments, results and errors as for kl_decode_step; a bad table
+ * entry up to the position's sets KL_DEVERR_PAGE, and its sequence is skipped
+ * as one with a bad position (KL_DEVERR_POSITION).  KL_ERR_UNSUPPORTED for a
+ * mixture of experts, and for a model loaded with a max_batch below
+ * kl_info.mfma_min_batch. */
+kl_status kl_decode_step_paged(kl_state *st, const int32_t *token_ids, const int32_t *positions,
+                               int32_t batch, const kl_paged_cache *cache,
+                               const kl_page_table *table, float *logits_out, float *hidden_out,
+                               void *stream);
+
 /* Bytes of ONE of the K or V buffers for the given batch and capacity
  * (0 if cfg is invalid). */
 size_t kl_kv_cache_bytes(const kl_config *cfg, int32_t batch, int32_t capacity);

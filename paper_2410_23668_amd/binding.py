@@ -42,7 +42,7 @@ EXPORTED = ["kl_load_model", "kl_model_create", "kl_model_set_layer", "kl_model_
             "kl_get_device_error",
             "kl_get_info", "kl_set_trace", "kl_read_stream", "kl_free_model", "kl_last_error",
             "kl_paged_append", "kl_paged_read", "kl_paged_attention",
-            "kl_paged_attention_workspace"]
+            "kl_paged_attention_workspace", "kl_decode_step_paged"]
 
 
 class kl_config(ctypes.Structure):
@@ -157,6 +157,8 @@ def lib():
     L.kl_paged_attention.argtypes = [pc, i32, pt, vp, pr, i32, ctypes.c_float, i32, pr, vp, vp,
                                      ctypes.c_size_t, vp, vp]
     L.kl_paged_attention.restype = i32
+    L.kl_decode_step_paged.argtypes = [vp, vp, vp, i32, pc, pt, vp, vp, vp]
+    L.kl_decode_step_paged.restype = i32
     L.kl_free_model.argtypes = [vp]
     L.kl_free_model.restype = None
     L.kl_last_error.argtypes = []
@@ -285,6 +287,13 @@ def kl_paged_attention(cache: kl_paged_cache, layer: int, table: kl_page_table, 
                        error: int | None, stream: int) -> None:
     _check(lib().kl_paged_attention(cache, layer, table, lengths, q, n_heads, scale, window, out,
                                     lse, workspace, workspace_bytes, error, stream))
+
+
+def kl_decode_step_paged(state: int, token_ids: int, positions: int, batch: int,
+                         cache: kl_paged_cache, table: kl_page_table, logits_out: int,
+                         hidden_out: int | None, stream: int) -> None:
+    _check(lib().kl_decode_step_paged(state, token_ids, positions, batch, cache, table, logits_out,
+                                      hidden_out, stream))
 
 
 def kl_free_model(state: int) -> None:

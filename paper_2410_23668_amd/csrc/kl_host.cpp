@@ -15,6 +15,7 @@
 #include "kl.h"
 #include "kl_error.h"
 #include "kl_internal.h"
+#include "kl_paged.h"
 
 using namespace kl;
 
@@ -51,6 +52,7 @@ struct kl_state {
     int nwg;
     LdsLayout lds;
     int own_max;                      // residual rows a workgroup owns, at most
+    uint8_t *paged;                   // scratch of paged steps (PagedScratch), or null: none run
 };
 
 namespace kl {
@@ -219,8 +221,23 @@ void bind_scratch(StepParams &P, uint8_t *base, const ScratchPlan &p, const kl_s
     P.qpart_stride = B * S.cfg.n_kv_heads * S.qkv_rg * kTileRows;
 }
 
+// Scratch of a paged step, for up to max_batch sequences: the attention's
+// workspace, a layer's new rows, and the sequences' positions and lengths.
+struct PagedScratch {
+    size_t off_counters, off_k, off_v, off_rows, total;
+    explicit PagedScratch(const kl_config &c) {
+        const size_t kv = align_up((size_t)c.max_batch * c.n_kv_heads * c.head_dim * 2, 256);
+        off_counters = kPagedPartBytes;
+        off_k = off_counters + align_up((size_t)c.max_batch * c.n_kv_heads * sizeof(unsigned), 256);
+        off_v = off_k + kv;
+        off_rows = off_v + kv;
+        total = off_rows + align_up((size_t)3 * c.max_batch * sizeof(int32_t), 256);
+    }
+};
+
 void free_state(kl_state *s) {
     if (!s) return;
+    if (s->paged) (void)hipFree(s->paged);
     if (s->arena) (void)hipFree(s->arena);
     if (s->rope) (void)hipFree(s->rope);
     if (s->scratch) (void)hipFree(s->scratch);
@@ -399,6 +416,12 @@ kl_status kl_model_create(const kl_config *cfg, kl_state **out) {
     TRY(hipMemsetAsync(S->err, 0, 256, s));
     S->epoch = reinterpret_cast<unsigned *>(reinterpret_cast<uint8_t *>(S->err) + 128);
     S->epoch_arrivals = reinterpret_cast<unsigned *>(reinterpret_cast<uint8_t *>(S->err) + 192);
+    if (c.max_batch >= S->lds.batched_from && c.n_experts <= 1) {
+        const size_t n = PagedScratch(c).total;
+        TRY(hipMalloc(&S->paged, n));
+        TRY(hipMemsetAsync(S->paged, 0, n, s));
+        S->scratch_bytes += n;
+    }
     const size_t key_bytes = align_up((size_t)kKeySlots * c.max_batch * sizeof(unsigned long long),
                                       16);
     TRY(hipMalloc(&S->keys, key_bytes));
@@ -761,6 +784,94 @@ kl_status kl_decode_greedy(kl_state *st, const int32_t *token_ids, const int32_t
     HIP_TRY(launch_emit_tokens(tokens_out + (size_t)(n_steps - 1) * batch, keys(n_steps - 1),
                                keys(0), batch, s));
     st->keys_clear = true;
+    return KL_OK;
+}
+
+kl_status kl_decode_step_paged(kl_state *st, const int32_t *token_ids, const int32_t *positions,
+                               int32_t batch, const kl_paged_cache *cache,
+                               const kl_page_table *table, float *logits_out, float *hidden_out,
+                               void *stream) {
+    const char *const who = "kl_decode_step_paged";
+    g_last_error.clear();
+    if (!st) return fail(KL_ERR_INVALID_ARGUMENT, "%s: state is NULL", who);
+    kl_status stt = check_paged_pool(cache, 0, table, who);
+    if (stt != KL_OK) return stt;
+    const kl_config &c = st->cfg;
+    if (cache->n_layers != c.n_layers || cache->n_kv_heads != c.n_kv_heads ||
+        cache->head_dim != c.head_dim || cache->device != st->device)
+        return fail(KL_ERR_INVALID_ARGUMENT, "%s: the cache's layers, KV heads, head_dim or device "
+                                             "are not the model's", who);
+    if (!st->paged)
+        return fail(KL_ERR_UNSUPPORTED, "%s: runs on the matrix-core path: dense models loaded with "
+                                        "max_batch >= %d", who, st->lds.batched_from);
+    if (table->batch < batch)
+        return fail(KL_ERR_INVALID_ARGUMENT, "%s: page table batch %d < batch %d", who, table->batch,
+                    batch);
+    // (the other arguments: as kl_decode_step's)
+    const PagedScratch off(c);
+    uint16_t *const rk = reinterpret_cast<uint16_t *>(st->paged + off.off_k);
+    uint16_t *const rv = reinterpret_cast<uint16_t *>(st->paged + off.off_v);
+    int32_t *const rows = reinterpret_cast<int32_t *>(st->paged + off.off_rows);
+    const int64_t room = (int64_t)table->max_pages * cache->page_size;
+    const kl_kv_cache kv = {rk, rv, batch, (int32_t)std::min<int64_t>(room, c.max_seq)};
+    stt = check_step_args(st, token_ids, positions, batch, &kv, logits_out, hidden_out,
+                          KL_MODE_PER_OP);
+    if (stt != KL_OK) return stt;
+
+    StepParams P = step_params(*st, st->scratch, plan_scratch(*st, c.max_batch, false), token_ids,
+                               rows, batch, &kv, logits_out, hidden_out);
+    P.batched = 1;
+    P.multi = 0;
+    P.lds_red = st->lds.red;
+    P.o_heads = P.nq;
+    P.rows_only = 1;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    StepRowsParams R{};
+    R.tokens = token_ids; R.positions = positions; R.batch = batch;
+    R.vocab = c.vocab; R.cap = kv.capacity;
+    R.n_pages = cache->n_pages; R.page_log2 = __builtin_ctz((unsigned)cache->page_size);
+    R.t = PagedTable{table->pages, batch, table->max_pages, table->stride};
+    R.step_pos = rows; R.append_pos = rows + c.max_batch; R.lengths = rows + 2 * c.max_batch;
+    R.error = st->err;
+    HIP_TRY(launch_paged_step_rows(R, s));
+
+    RowParams W{};
+    W.t = R.t;
+    W.positions = R.append_pos; W.rows = batch;
+    W.k = rk; W.v = rv; W.k_type = W.v_type = KL_DTYPE_BF16;
+    W.k_row = W.v_row = (long long)P.nkv * P.d;
+    W.k_head = W.v_head = P.d;
+    W.k_vec = W.v_vec = true;
+    W.error = st->err;
+    AttnParams A{};
+    A.t = R.t;
+    A.lengths = R.lengths;
+    A.q = P.q; A.q_type = KL_DTYPE_FP32;
+    A.out = P.acto; A.out_lo = P.acto_lo; A.out_type = KL_DTYPE_BF16;
+    A.nq = P.nq; A.group = P.group;
+    A.q_row = A.out_row = (long long)P.nq * P.d;
+    A.q_head = A.out_head = P.d;
+    A.q_vec = A.out_vec = true;
+    A.scale = (float)(1.0 / std::sqrt((double)P.d));
+    A.parts = reinterpret_cast<float *>(st->paged);
+    A.arrived = reinterpret_cast<unsigned *>(st->paged + off.off_counters);
+    A.error = st->err;
+
+    const int lds = st->lds.bytes;
+    const auto phase = [&](int l0, int l1, int ph) {
+        return launch_step(P, l0, l1, ph, launch_waits_inside(ph, true), lds, s);
+    };
+    HIP_TRY(phase(0, 0, kPhEmbed));
+    for (int l = 0; l < P.L; ++l) {
+        HIP_TRY(phase(l, l + 1, kPhQkv));
+        W.c = A.c = paged_layer(*cache, l);
+        HIP_TRY(launch_paged_append(W, s));
+        HIP_TRY(launch_paged_attention(A, s));
+        HIP_TRY(phase(l, l + 1, kPhOproj));
+        HIP_TRY(phase(l, l + 1, kPhGateUp));
+        HIP_TRY(phase(l, l + 1, kPhDown));
+    }
+    HIP_TRY(phase(0, 0, kPhHead));
     return KL_OK;
 }
 

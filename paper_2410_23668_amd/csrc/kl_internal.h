@@ -61,6 +61,8 @@ struct StepParams {
     int B;
     uint16_t *kc, *vc;         // [L][kv_batch][nkv][cap][d]
     int kv_batch, cap;
+    int rows_only;             // matrix-core path: kc, vc [B][nkv][d] take the step's new rows
+                               // of one layer (a paged step, whose attention is another kernel)
     float *logits, *hidden_out;
     // scratch
     long long *xf;             // [max_batch][Hp] residual stream, fixed point (2^-32 units)

@@ -43,6 +43,19 @@ struct RowParams {
     bool k_vec, v_vec;               // 8 elements of a head may be moved as 16-byte words
     int32_t *error;
 };
+// A paged step's sequences: position and length of each for its launches.
+// Sequence b attends lengths[b] positions and its row goes to append_pos[b] (-1:
+// none); step_pos[b] is its position, -1 where its pages are bad (checked up to
+// that position's; KL_DEVERR_PAGE).
+struct StepRowsParams {
+    const int32_t *tokens, *positions;
+    int vocab, cap, n_pages, page_log2, batch;
+    PagedTable t;
+    int32_t *step_pos, *append_pos, *lengths;
+    int32_t *error;
+};
+hipError_t launch_paged_step_rows(const StepRowsParams &p, hipStream_t stream);
+
 hipError_t launch_paged_append(const RowParams &p, hipStream_t stream);
 hipError_t launch_paged_read(const RowParams &p, hipStream_t stream);
 
@@ -58,6 +71,7 @@ struct AttnParams {
     long long q_row, q_head, out_row, out_head;
     float scale;
     int window;
+    uint16_t *out_lo;                // with bf16 'out': its second bf16 term (a step's attention)
     float *lse;
     float *parts;                    // workspace: [workgroup][2][group][d + 2]
     unsigned *arrived;               // workspace: [batch][nkv], zero between calls
@@ -66,5 +80,10 @@ struct AttnParams {
 hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream);
 hipError_t launch_paged_attention_d64(const AttnParams &p, hipStream_t stream);
 hipError_t launch_paged_attention_d128(const AttnParams &p, hipStream_t stream);
+
+// Host checks shared by the entry points (kl_paged_host.cpp).
+kl_status check_paged_pool(const kl_paged_cache *c, int32_t layer, const kl_page_table *t,
+                           const char *who);
+PagedLayer paged_layer(const kl_paged_cache &c, int32_t layer);
 
 }  // namespace kl

@@ -229,6 +229,31 @@ hipError_t launch_paged_read(const RowParams &p, hipStream_t stream) {
     return wide ? read_for<64, true>(p, stream) : read_for<64, false>(p, stream);
 }
 
+// One wave per sequence.
+__global__ void __launch_bounds__(64) kl_paged_step_rows_kernel(StepRowsParams p) {
+    const int b = blockIdx.x, lane = threadIdx.x;
+    const int t = p.tokens[b], pos = p.positions[b];
+    const bool in = pos >= 0 && pos < p.cap;
+    bool bad = false;
+    if (in)
+        for (int i = lane; i <= pos >> p.page_log2; i += 64) {
+            const int page = p.t.pages[(long long)b * p.t.stride + i];
+            bad = bad || page < 0 || page >= p.n_pages;
+        }
+    bad = __any(bad);
+    if (lane != 0) return;
+    if (bad) flag_error(p.error, KL_DEVERR_PAGE);
+    const bool ok = in && !bad && t >= 0 && t < p.vocab;
+    p.step_pos[b] = bad ? -1 : pos;
+    p.append_pos[b] = ok ? pos : -1;
+    p.lengths[b] = ok ? pos + 1 : 0;
+}
+
+hipError_t launch_paged_step_rows(const StepRowsParams &p, hipStream_t stream) {
+    hipLaunchKernelGGL(kl_paged_step_rows_kernel, dim3(p.batch), dim3(64), 0, stream, p);
+    return hipGetLastError();
+}
+
 hipError_t launch_paged_attention(const AttnParams &p, hipStream_t stream) {
     return p.c.d == 128 ? launch_paged_attention_d128(p, stream)
                         : launch_paged_attention_d64(p, stream);

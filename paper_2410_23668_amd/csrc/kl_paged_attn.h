@@ -398,6 +398,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             store1(p.out, p.out_type, at, x0);
             store1(p.out, p.out_type, at + 1, x1);
         }
+        if (Full && p.out_lo) {
+            store1(p.out_lo, KL_DTYPE_BF16, at, x0 - bf2f(f2bf(x0)));
+            store1(p.out_lo, KL_DTYPE_BF16, at + 1, x1 - bf2f(f2bf(x1)));
+        }
         if (p.lse && dd == 0) write_lse(b, g, h, a.m, a.l);
     };
 
@@ -622,9 +626,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                     float v[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] = r[dd + j] * inv;
-                    store8(reinterpret_cast<uint8_t *>(p.out) +
-                               (a.b * p.out_row + (a.g * G + h) * p.out_head + dd) * out_bytes,
-                           p.out_type, p.out_vec, v);
+                    const long long at = a.b * p.out_row + (a.g * G + h) * p.out_head + dd;
+                    store8(reinterpret_cast<uint8_t *>(p.out) + at * out_bytes, p.out_type,
+                           p.out_vec, v);
+                    if (Full && p.out_lo) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] -= bf2f(f2bf(v[j]));
+                        store8(p.out_lo + at, KL_DTYPE_BF16, p.out_vec, v);
+                    }
                     if (p.lse && dd == 0) write_lse(a.b, a.g, h, r[D], r[D + 1]);
                 }
                 __builtin_amdgcn_wave_barrier();
@@ -811,7 +820,7 @@ static hipError_t launch_copies(const AttnParams &p, hipStream_t stream) {
 }
 template <int D>
 static hipError_t launch_attention_for(const AttnParams &p, hipStream_t stream) {
-    const bool full = p.q_type != KL_DTYPE_BF16 || p.out_type == KL_DTYPE_FP32;
+    const bool full = p.q_type != KL_DTYPE_BF16 || p.out_type == KL_DTYPE_FP32 || p.out_lo;
     if (p.c.e4m3) return full ? launch_copies<D, true, true>(p, stream) : launch_copies<D, true, false>(p, stream);
     return full ? launch_copies<D, false, true>(p, stream) : launch_copies<D, false, false>(p, stream);
 }

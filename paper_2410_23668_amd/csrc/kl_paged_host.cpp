@@ -32,8 +32,12 @@ kl_status check_cache(const kl_paged_cache *c, const char *who) {
     return KL_OK;
 }
 
-kl_status check_pool(const kl_paged_cache *c, int32_t layer, const kl_page_table *t,
-                     const char *who) {
+}  // namespace
+
+namespace kl {
+
+kl_status check_paged_pool(const kl_paged_cache *c, int32_t layer, const kl_page_table *t,
+                           const char *who) {
     const kl_status st = check_cache(c, who);
     if (st != KL_OK) return st;
     if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))
@@ -53,6 +57,25 @@ kl_status check_pool(const kl_paged_cache *c, int32_t layer, const kl_page_table
         return fail(KL_ERR_UNSUPPORTED, "%s: max_pages * page_size above 2^30", who);
     return KL_OK;
 }
+
+PagedLayer paged_layer(const kl_paged_cache &c, int32_t layer) {
+    PagedLayer p{};
+    p.e4m3 = c.dtype == KL_DTYPE_E4M3;
+    p.n_pages = c.n_pages; p.nkv = c.n_kv_heads; p.page_log2 = log2_of(c.page_size); p.d = c.head_dim;
+    const size_t rows = (size_t)c.n_pages * c.n_kv_heads * c.page_size;
+    const size_t off = (size_t)layer * rows * c.head_dim * (p.e4m3 ? 1 : 2);
+    p.k = reinterpret_cast<uint8_t *>(c.k) + off;
+    p.v = reinterpret_cast<uint8_t *>(c.v) + off;
+    if (p.e4m3) {
+        p.ks = c.k_scale + layer * rows;
+        p.vs = c.v_scale + layer * rows;
+    }
+    return p;
+}
+
+}  // namespace kl
+
+namespace {
 
 kl_status check_device(const kl_paged_cache *c, const char *who) {
     int dev = -1;
@@ -85,21 +108,6 @@ bool vector_rows(const kl_rows &r, int64_t rows, int heads) {
            (heads == 1 || r.head_stride * el % 16 == 0);
 }
 
-PagedLayer layer_of(const kl_paged_cache &c, int32_t layer) {
-    PagedLayer p{};
-    p.e4m3 = c.dtype == KL_DTYPE_E4M3;
-    p.n_pages = c.n_pages; p.nkv = c.n_kv_heads; p.page_log2 = log2_of(c.page_size); p.d = c.head_dim;
-    const size_t rows = (size_t)c.n_pages * c.n_kv_heads * c.page_size;
-    const size_t off = (size_t)layer * rows * c.head_dim * (p.e4m3 ? 1 : 2);
-    p.k = reinterpret_cast<uint8_t *>(c.k) + off;
-    p.v = reinterpret_cast<uint8_t *>(c.v) + off;
-    if (p.e4m3) {
-        p.ks = c.k_scale + layer * rows;
-        p.vs = c.v_scale + layer * rows;
-    }
-    return p;
-}
-
 PagedTable table_of(const kl_page_table &t) {
     return PagedTable{t.pages, t.batch, t.max_pages, t.stride};
 }
@@ -108,7 +116,7 @@ PagedTable table_of(const kl_page_table &t) {
 kl_status row_params(const kl_paged_cache *cache, int32_t layer, const kl_page_table *table,
                      const int32_t *seq, const int32_t *positions, int64_t rows, const kl_rows *k,
                      const kl_rows *v, int32_t *error, bool output, const char *who, RowParams *p) {
-    kl_status st = check_pool(cache, layer, table, who);
+    kl_status st = check_paged_pool(cache, layer, table, who);
     if (st != KL_OK) return st;
     if (rows < 0 || rows > INT32_MAX)
         return fail(KL_ERR_INVALID_ARGUMENT, "%s: rows %lld outside [0, 2^31)", who, (long long)rows);
@@ -123,7 +131,7 @@ kl_status row_params(const kl_paged_cache *cache, int32_t layer, const kl_page_t
         if (st != KL_OK) return st;
         st = check_rows(v, rows, cache->n_kv_heads, cache->head_dim, output, "v", who);
         if (st != KL_OK) return st;
-        *p = RowParams{layer_of(*cache, layer), table_of(*table), seq, positions, rows, k->data,
+        *p = RowParams{paged_layer(*cache, layer), table_of(*table), seq, positions, rows, k->data,
                        v->data, k->dtype, v->dtype, k->row_stride, k->head_stride, v->row_stride,
                        v->head_stride, vector_rows(*k, rows, cache->n_kv_heads),
                        vector_rows(*v, rows, cache->n_kv_heads), error};
@@ -176,7 +184,7 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
                              void *stream) {
     const char *const who = "kl_paged_attention";
     g_last_error.clear();
-    kl_status st = check_pool(cache, layer, table, who);
+    kl_status st = check_paged_pool(cache, layer, table, who);
     if (st != KL_OK) return st;
     const kl_paged_cache &c = *cache;
     const int B = table->batch;
@@ -208,7 +216,7 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     st = check_device(cache, who);
     if (st != KL_OK) return st;
     AttnParams p{};
-    p.c = layer_of(c, layer); p.t = table_of(*table);
+    p.c = paged_layer(c, layer); p.t = table_of(*table);
     p.lengths = lengths;
     p.q = q->data; p.q_type = q->dtype; p.q_row = q->row_stride; p.q_head = q->head_stride;
     p.q_vec = vector_rows(*q, B, n_heads);

@@ -1913,6 +1913,9 @@ __device__ __forceinline__ void qkv_store(const StepParams &P, int l, int b, int
     const int p = pos_of<LL>(P, b);
     const bool ok = ok_of<LL>(P, b);
     unsigned long long *kvl = LL ? P.kv_ll + ((size_t)b * P.nkv + g) * d : nullptr;
+    const auto row = [&]() {
+        return !LL && P.rows_only ? (size_t)b * P.nkv + g : kv_row(P, l, b, g) + p;
+    };
     if (lr < (G + 1) * d) {
         const int i = (lr % d) >> 1;
         const float2 cs = rope(p, i);
@@ -1930,7 +1933,7 @@ __device__ __forceinline__ void qkv_store(const StepParams &P, int l, int b, int
         } else {
             const uint16_t k0 = f2bf(u0), k1 = f2bf(u1);
             if (ok) {
-                uint16_t *kk = P.kc + (kv_row(P, l, b, g) + p) * d;
+                uint16_t *kk = P.kc + row() * d;
                 st_dev_u16(kk + i, k0);
                 st_dev_u16(kk + i + half, k1);
             }
@@ -1940,7 +1943,7 @@ __device__ __forceinline__ void qkv_store(const StepParams &P, int l, int b, int
         const int j = lr - (G + 1) * d;
         const unsigned v01 = (unsigned)f2bf(y0) | ((unsigned)f2bf(y1) << 16);
         if (ok) {
-            uint16_t *vv = P.vc + (kv_row(P, l, b, g) + p) * d;
+            uint16_t *vv = P.vc + row() * d;
             st_dev_u32(reinterpret_cast<unsigned *>(vv + j), v01);
         }
         if (LL) st_ll(kvl + half + j / 2, v01, tag);

@@ -104,6 +104,21 @@ class GpuModel:
                           logits.data_ptr(), hidden.data_ptr() if hidden is not None else None,
                           stream_handle(stream), mode)
 
+    def step_paged(self, tokens: torch.Tensor, positions: torch.Tensor, pool: "PagedKvCache",
+                   table: torch.Tensor, logits: torch.Tensor, hidden: torch.Tensor | None = None,
+                   stream: torch.cuda.Stream | None = None) -> None:
+        """step() over a paged cache: row b of the table holds sequence b's pages."""
+        assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
+        assert logits.dtype == torch.float32 and logits.is_contiguous()
+        B = tokens.numel()
+        assert logits.shape == (B, self.model_cfg["vocab"])
+        if hidden is not None:
+            assert hidden.dtype == torch.float32 and hidden.shape == (B, self.model_cfg["hidden"])
+        kb.kl_decode_step_paged(self.state, tokens.data_ptr(), positions.data_ptr(), B, pool.c,
+                                pool._table(table), logits.data_ptr(),
+                                hidden.data_ptr() if hidden is not None else None,
+                                stream_handle(stream))
+
     def greedy(self, tokens: torch.Tensor, positions: torch.Tensor, kv: "KvCache", n_steps: int,
                tokens_out: torch.Tensor, logits: torch.Tensor, mode: int,
                stream: torch.cuda.Stream | None = None) -> None:

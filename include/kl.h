@@ -364,8 +364,8 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
  * positions[b]'s slot of every layer (as kl_paged_append) and attends over
  * positions 0..positions[b] (as kl_paged_attention), so an e4m3 pool halves
  * the cache that a step reads.  It runs on the matrix-core path at every batch,
- * one launch per operator group with the two operators in place of the
- * attention's (6 L + 3 dispatches).
+ * two launches per layer with the two operators' between them (4 L + 1
+ * dispatches).
  *   cache    of the model's n_layers, n_kv_heads, head_dim and device
  *   table    batch >= the step's; positions are < max_pages * page_size and
  *            < max_seq

@@ -861,17 +861,15 @@ kl_status kl_decode_step_paged(kl_state *st, const int32_t *token_ids, const int
     const auto phase = [&](int l0, int l1, int ph) {
         return launch_step(P, l0, l1, ph, launch_waits_inside(ph, true), lds, s);
     };
-    HIP_TRY(phase(0, 0, kPhEmbed));
+    // the phases between two layers' attentions in as few launches as the step
+    // kernel's order of phases allows
     for (int l = 0; l < P.L; ++l) {
-        HIP_TRY(phase(l, l + 1, kPhQkv));
+        HIP_TRY(phase(l, l + 1, kPhQkv | (l == 0 ? kPhEmbed : 0)));
         W.c = A.c = paged_layer(*cache, l);
         HIP_TRY(launch_paged_append(W, s));
         HIP_TRY(launch_paged_attention(A, s));
-        HIP_TRY(phase(l, l + 1, kPhOproj));
-        HIP_TRY(phase(l, l + 1, kPhGateUp));
-        HIP_TRY(phase(l, l + 1, kPhDown));
+        HIP_TRY(phase(l, l + 1, kPhOproj | kPhGateUp | kPhDown | (l + 1 == P.L ? kPhHead : 0)));
     }
-    HIP_TRY(phase(0, 0, kPhHead));
     return KL_OK;
 }
 

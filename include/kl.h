@@ -336,6 +336,7 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  * head h with KV head h / (n_heads / n_kv_heads).
  *   lengths    dev int32 [batch]; 0: no position (a padded batch): the output
  *              row is zero and its lse -infinity
+ *              (batch * n_kv_heads * max_pages * page_size <= 2^35)
  *   q, out     n_heads heads; n_heads a multiple of n_kv_heads, at most 16
  *              times as many
  *   scale      finite

@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     const bool few = B <= 64;
     if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
     int len_own = 0, upto = 0, most = 0, T;
-    auto wave_scan = [&](int v) {   // inclusive sum over the lanes (zero past B)
+    auto wave_scan = [&](int v) {   // inclusive sum over the first B lanes
         for (int off = 1; off < 64 && off < B; off <<= 1) {
             const int o = from_lane(v, max(lane - off, 0));
             v += lane >= off ? o : 0;

@@ -199,9 +199,9 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     if (!lengths || !aligned(lengths, 4) || !aligned(lse, 4) || !aligned(error, 4))
         return fail(KL_ERR_INVALID_ARGUMENT, "%s: lengths must not be NULL, and int32/fp32 buffers "
                                              "4-byte aligned", who);
-    if ((int64_t)B * c.n_kv_heads * (((int64_t)table->max_pages * c.page_size + 31) / 32 + 1) >
-        INT32_MAX)
-        return fail(KL_ERR_UNSUPPORTED, "%s: batch * n_kv_heads * max_pages * page_size too large",
+    // (tiles, of 32 positions at least, are counted in 32 bits)
+    if ((int64_t)B * c.n_kv_heads * (((int64_t)table->max_pages * c.page_size + 31) / 32) > (1 << 30))
+        return fail(KL_ERR_UNSUPPORTED, "%s: batch * n_kv_heads * max_pages * page_size above 2^35",
                     who);
     st = check_rows(q, B, n_heads, c.head_dim, false, "q", who);
     if (st != KL_OK) return st;

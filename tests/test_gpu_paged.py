@@ -583,6 +583,94 @@ def test_the_contiguous_cache_and_pages():
         assert not b[:, 1].any() and not b[:, 0, :, n:].any()
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("window", [0, 19])
+def test_more_sequences_than_a_wave_has_lanes(cache, window):
+    # lengths of all kinds, empty and bad ones among them, bad pages of one
+    g = gen(50)
+    page, kv, nq, d, B = 8, 3, 12, 64, 150
+    lengths = [(53 * i * i) % 97 if i % 9 else 0 for i in range(B)]
+    n_pages = sum(-(-n // page) for n in lengths)
+    pool = make_pool(1, n_pages, kv, page, d, cache, g)
+    table = make_table(lengths, page, n_pages, g, extra=0)
+    q = torch.randn(B, nq, d, generator=g)
+    want = attention64(values(pool, "k"), values(pool, "v"), table, lengths, q, page, d ** -0.5, window)
+    ws = pool.workspace(B)
+    out, lse = run_attention(pool, table, lengths, q, page, window=window, ws=ws)
+    check_attention(out, lse, want)
+    assert pool.device_error() == 0
+    lens, bad = list(lengths), table.clone()
+    lens[70] = -1
+    lens[149] = table.shape[1] * page + 1
+    victim = max(range(71, 149), key=lambda b: lengths[b])
+    bad[victim, (lengths[victim] - 1) // page] = n_pages
+    out, lse = run_attention(pool, bad, lens, q, page, window=window, ws=ws)
+    assert pool.device_error() == kb.KL_DEVERR_PAGE | kb.KL_DEVERR_POSITION
+    keep = torch.tensor([b for b in range(B) if b not in (70, 149, victim)])
+    assert torch.isnan(out[[70, 149, victim]]).all() and torch.isnan(lse[[70, 149, victim]]).all()
+    check_attention(out[keep.cuda()], lse[keep.cuda()], [w[keep] for w in want])
+
+
+def test_the_largest_batch_and_group():
+    g = gen(51)
+    page, kv, nq, d, B = 16, 1, 16, 128, 4096
+    lengths = [(i * 7) % 33 for i in range(B)]
+    pool = make_pool(1, 400, kv, page, d, E4M3, g)
+    table = torch.randint(0, 400, (B, 3), generator=g).to(torch.int32)   # (pages shared by many)
+    q = torch.randn(B, nq, d, generator=g).to(BF16)
+    out, lse = run_attention(pool, table, lengths, q, page)
+    pick = torch.cat([torch.arange(40), torch.randint(0, B, (60,), generator=g), torch.arange(B - 40, B)])
+    want = attention64(values(pool, "k"), values(pool, "v"), table[pick],
+                       [lengths[int(i)] for i in pick], q[pick], page, d ** -0.5)
+    check_attention(out[pick.cuda()], lse[pick.cuda()], want)
+    assert torch.isfinite(out).all() and pool.device_error() == 0
+
+
+def test_sequences_that_share_their_pages_agree():
+    g = gen(52)
+    page, kv, d = 32, 2, 128
+    pool = make_pool(1, 40, kv, page, d, E4M3, g)
+    one = make_table([1000], page, 40, g)
+    q = torch.randn(1, 8, d, generator=g)
+    a, la = run_attention(pool, one.expand(5, -1).contiguous(), [1000, 17, 1000, 0, 1000],
+                          q.expand(5, -1, -1).contiguous(), page)
+    want = attention64(values(pool, "k"), values(pool, "v"), one, [1000], q, page, d ** -0.5)
+    for b in (0, 2, 4):
+        check_attention(a[b:b + 1], la[b:b + 1], want)
+    # one query for all of them, by a row stride of zero
+    b_, lb = run_attention(pool, one.expand(5, -1).contiguous(), [1000, 17, 1000, 0, 1000],
+                           q.cuda().expand(5, -1, -1), page)
+    assert torch.equal(a, b_) and torch.equal(la, lb)
+
+
+def test_two_streams_append_and_attend_at_once():
+    """Rows of some sequences are written while others are attended over."""
+    g = gen(53)
+    page, kv, nq, d = 16, 4, 16, 128
+    pool = make_pool(1, 600, kv, page, d, E4M3, g)
+    table = make_table([4000, 3000], page, 600, g).cuda()
+    q = torch.randn(2, nq, d, generator=g).cuda()
+    n = torch.tensor([4000, 0], dtype=torch.int32).cuda()
+    outs = [torch.empty(2, nq, d, device="cuda") for _ in range(2)]
+    wss = [pool.workspace(2) for _ in range(2)]
+    rows = torch.randn(3000, kv, d, generator=g).to(BF16).cuda()
+    pos = torch.arange(3000, dtype=torch.int32).cuda()
+    seq = torch.ones_like(pos)
+    pool.attention(0, table, n, q, outs[0], wss[0])
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        pool.append(0, table, pos, rows, rows, seq=seq, stream=s1)
+        pool.attention(0, table, n, q, outs[1], wss[1], stream=s2)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    back = [torch.empty(3000, kv, d, device="cuda") for _ in range(2)]
+    pool.read(0, table, pos, back[0], back[1], seq=seq)
+    codes, scale = e4m3_rows(rows)
+    want = codes.view(E4M3).float() * torch.exp2(scale.float() - 127)[..., None]
+    assert torch.equal(back[0].cpu(), want) and torch.equal(back[1].cpu(), want)
+
+
 def test_wrong_device_index_is_refused():
     pool = make_pool(1, 2, 1, 8, 64, BF16, gen(1))
     pool.c.device = 1

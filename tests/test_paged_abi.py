@@ -90,6 +90,7 @@ def call_attention(c=cache(), layer=0, t=table(), lengths=A, q=rows(), heads=8, 
 
 @pytest.mark.parametrize("over,status,msg", POOL + [
     (dict(t=table(batch=4097)), kb.KL_ERR_UNSUPPORTED, "4096"),
+    (dict(t=table(batch=4096, max_pages=1 << 18, stride=1 << 18)), kb.KL_ERR_UNSUPPORTED, "2^35"),
     (dict(heads=0), kb.KL_ERR_INVALID_ARGUMENT, "n_heads"),
     (dict(heads=10), kb.KL_ERR_INVALID_ARGUMENT, "multiple"),
     (dict(heads=4 * 17), kb.KL_ERR_UNSUPPORTED, "17 query heads"),

@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     // wave has lanes for all (no wait for the other waves: 1 us less), else in LDS.
     const bool few = B <= 64;
     if (lane < 2) unit[2 * wave + lane] = -1;   // (read behind a barrier)
-    int len_own = 0, upto = 0, most = 0, T;
+    int len_own = 0, tiles_own = 0, upto = 0, T;
     auto wave_scan = [&](int v) {   // inclusive sum over the first B lanes
         for (int off = 1; off < 64 && off < B; off <<= 1) {
             const int o = from_lane(v, max(lane - off, 0));
@@ -186,9 +186,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     };
     if (few) {
         if (lane < B) len_own = checked(p.lengths[lane]);
-        const int own = lane < B ? tiles_of(len_own) : 0;
-        upto = wave_scan(own);
-        most = uni((int)wave_max((float)own));   // (exact below 2^24; above, far from any bound)
+        tiles_own = lane < B ? tiles_of(len_own) : 0;
+        upto = wave_scan(tiles_own);
         T = __builtin_amdgcn_readlane(upto, B - 1) * nkv;
     } else {
         if (tid == 0) pre[0] = 0;
@@ -221,18 +220,42 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         return checked(reinterpret_cast<const KL_KARG int32_t *>(
             reinterpret_cast<uint64_t>(p.lengths))[b]);
     };
-    // the workgroup's share [X0, X1): a unit of its own (unit_shares), or an
-    // equal share, with a workgroup for every kAttnWaves tiles
-    const int wg = blockIdx.x;
-    const bool by_unit = few && unit_shares(B * nkv, gridDim.x, most, T, kAttnWaves);
-    const Shares sh(T, by_unit ? B * nkv : min((int)gridDim.x, (T + kAttnWaves - 1) / kAttnWaves));
-    if (wg >= sh.np) return;
-    int X0, X1;
-    if (by_unit) {
-        const int b = uni(wg / nkv), g = wg - b * nkv, nt = before(b + 1) - before(b);
-        X0 = before(b) * nkv + g * nt;
-        X1 = X0 + nt;
-    } else {
+    // The workgroup's share [X0, X1): of one unit (unit_shares), or an equal
+    // share, with a workgroup for every kAttnWaves tiles.  Units of several
+    // workgroups: the one that the share begins inside of, and the one that
+    // begins in the share and goes on behind it; their numbers of workgroups,
+    // and the first one's first.
+    const int wg = blockIdx.x, groups = gridDim.x;
+    int X0 = 0, X1 = 0, sent0 = -1, sent1 = -1, from0 = 0, count0 = 0, count1 = 0;
+    bool by_unit = false;
+    if (few && B * nkv <= groups) {
+        const int equal = uni(equal_rounds(T, groups, kAttnWaves));
+        const int most = uni((int)wave_max((float)tiles_own));   // (exact where it matters: below 2^24)
+        for (int r = equal; r <= equal + kUnitRounds && !by_unit; ++r) {
+            const int own = unit_groups(tiles_own, r, kAttnWaves), to = wave_scan(own);
+            by_unit = unit_shares(__builtin_amdgcn_readlane(to, B - 1) * nkv, groups, most, r, equal,
+                                  kAttnWaves);
+            if (!by_unit) continue;
+            if (wg >= __builtin_amdgcn_readlane(to, B - 1) * nkv) return;
+            const int b = __popcll(__ballot(lane < B && to * nkv <= wg));
+            const int n = __builtin_amdgcn_readlane(own, b), nt = __builtin_amdgcn_readlane(tiles_own, b);
+            const int i = wg - (__builtin_amdgcn_readlane(to, b) - n) * nkv;
+            const int g = n == 1 ? i : uni(i / n), j = i - g * n;
+            X0 = before(b) * nkv + g * nt;
+            X1 = X0 + nt;
+            if (n > 1) {
+                const Shares unit_sh(nt, n);
+                X1 = uni(X0 + unit_sh.first(j + 1));
+                X0 = uni(X0 + unit_sh.first(j));
+            }
+            if (j > 0) sent0 = b * nkv + g, from0 = wg - j, count0 = n;
+            else if (n > 1) sent1 = b * nkv + g, count1 = n;
+        }
+    }
+    Shares sh(1, 1);
+    if (!by_unit) {
+        sh = Shares(T, min(groups, (T + kAttnWaves - 1) / kAttnWaves));
+        if (wg >= sh.np) return;
         X0 = uni(sh.first(wg));
         X1 = uni(sh.first(wg + 1));
     }
@@ -558,11 +581,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         }
     };
 
-    // Units of several workgroups: the one that the share begins inside of, and
-    // the one that begins in the share and goes on behind it; each one's first
-    // workgroup and their number.
-    int sent0 = -1, sent1 = -1, from0 = 0, count0 = 0, count1 = 0;
-    auto find_shared = [&]() {
+    auto find_shared = [&]() {   // (equal shares: sent0 and what goes with it)
         if (by_unit) return;
         const At h = find(X0), e = find(X1 - 1);
         const int hb = X0 - h.t, eb = X1 - 1 - e.t;

@@ -43,14 +43,25 @@ struct Shares {
     }
 };
 
-// Where a workgroup can have a unit to itself, the parts need not meet in
-// memory (about 4 us), for at most kUnitRounds more rounds of its waves than
-// an equal share has (a round, a tile for each wave, is about 2 us).
+// Where it can be had at no cost, a workgroup has tiles of one unit only: each
+// unit gets whole workgroups, as many as make shares of at most r rounds (a
+// round is a tile for each of the workgroup's waves, about 2 us).  A workgroup
+// then hands on one part and not two, and units of r rounds at most need no
+// part in memory at all, which is worth about 4 us: for those r may be up to
+// kUnitRounds above what equal shares have.
 constexpr int kUnitRounds = 2;
-KL_HD inline bool unit_shares(int units, int groups, int most, int T, int waves) {
-    const int np = (T + waves - 1) / waves < groups ? (T + waves - 1) / waves : groups;
-    const int equal = ((T + np - 1) / np + waves - 1) / waves;
-    return units <= groups && (most + waves - 1) / waves <= equal + kUnitRounds;
+KL_HD inline int equal_rounds(int T, int groups, int waves) {
+    const int each = (T + groups - 1) / groups;
+    return (each + waves - 1) / waves;
+}
+// workgroups of a unit of nt tiles
+KL_HD inline int unit_groups(int nt, int r, int waves) {
+    const int rounds = (nt + waves - 1) / waves;
+    return r == 1 ? rounds : (rounds + r - 1) / r;
+}
+// whether 'need' workgroups so, for units of at most 'most' tiles, are taken
+KL_HD inline bool unit_shares(int need, int groups, int most, int r, int equal, int waves) {
+    return need <= groups && (r == equal || most <= r * waves);
 }
 
 }  // namespace kl

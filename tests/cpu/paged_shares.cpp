@@ -41,10 +41,24 @@ void walk(const std::vector<int> &lengths, int nkv, int window, int NK, int grid
             T += n;
             if (n > most) most = n;
         }
-    const int units = B * nkv;
-    const bool by_unit = may_by_unit && unit_shares(units, grid, most, T, kWaves);
+    const int units = B * nkv, equal = equal_rounds(T, grid, kWaves);
+    bool by_unit = false;
+    std::vector<int> unit_wg, part_wg, groups_of(units);   // by workgroup; by unit
+    for (int r = equal; may_by_unit && r <= equal + kUnitRounds && !by_unit; ++r) {
+        int need = 0;
+        for (int u = 0; u < units; ++u) need += groups_of[u] = unit_groups(nt[u], r, kWaves);
+        by_unit = unit_shares(need, grid, most, r, equal, kWaves);
+        if (by_unit)
+            for (int u = 0; u < units; ++u)
+                for (int j = 0; j < groups_of[u]; ++j) {
+                    unit_wg.push_back(u);
+                    part_wg.push_back(j);
+                }
+    }
     const int want = (T + kWaves - 1) / kWaves < grid ? (T + kWaves - 1) / kWaves : grid;
-    const Shares sh(T, by_unit ? units : want);
+    const Shares sh(T, want);
+    const int np = by_unit ? (int)unit_wg.size() : sh.np;
+    check(np <= grid, "workgroups", np, grid);
     std::vector<int> unit_of(T);
     for (int u = 0; u < units; ++u)
         for (int i = 0; i < nt[u]; ++i) unit_of[first_of[u] + i] = u;
@@ -52,12 +66,21 @@ void walk(const std::vector<int> &lengths, int nkv, int window, int NK, int grid
     std::vector<int> seen(T, 0);
     std::map<int, std::set<std::pair<int, int>>> parts;   // unit -> (workgroup, slot) in memory
     std::map<int, int> arrivals, counts, writes;          // unit -> ...
-    for (int wg = 0; wg < sh.np; ++wg) {
-        int X0, X1;
-        if (by_unit) X0 = first_of[wg], X1 = X0 + nt[wg];
-        else X0 = sh.first(wg), X1 = sh.first(wg + 1);
-        check(X1 > X0, "a share", wg, sh.np);
+    std::vector<int> first_wg(units, -1);   // of units of several workgroups
+    for (int wg = 0; wg < np; ++wg) {
+        int X0 = 0, X1 = 0;
         int sent0 = -1, sent1 = -1, from0 = 0, count0 = 0, count1 = 0;
+        if (by_unit) {
+            const int u = unit_wg[wg], j = part_wg[wg], n = groups_of[u];
+            const Shares s(nt[u], n);
+            X0 = first_of[u] + s.first(j);
+            X1 = first_of[u] + s.first(j + 1);
+            if (j > 0) sent0 = u, from0 = wg - j, count0 = n;
+            else if (n > 1) sent1 = u, count1 = n;
+        } else {
+            X0 = sh.first(wg), X1 = sh.first(wg + 1);
+        }
+        check(X1 > X0, "a share", wg, np);
         if (!by_unit) {
             const int hu = unit_of[X0], eu = unit_of[X1 - 1];
             const int hb = first_of[hu], eb = first_of[eu];
@@ -100,12 +123,13 @@ void walk(const std::vector<int> &lengths, int nkv, int window, int NK, int grid
                 parts[u].insert({wg, u == sent1});
             }
         }
+        if (sent1 >= 0) first_wg[sent1] = wg;
         if (sent0 >= 0) {
             check(in_lds.count(sent0), "the part of an earlier unit", wg, sent0);
             ++arrivals[sent0];
             const int had = counts.emplace(sent0, count0).first->second;
             check(had == count0, "the same count everywhere", had, count0);
-            check(from0 == sh.of(first_of[sent0]), "first workgroup", from0, wg);
+            check(from0 == first_wg[sent0], "first workgroup", from0, wg);
         }
         if (sent1 >= 0) {
             check(in_lds.count(sent1), "the part of a unit that goes on", wg, sent1);
@@ -119,7 +143,7 @@ void walk(const std::vector<int> &lengths, int nkv, int window, int NK, int grid
         check((writes.count(u) ? writes[u] : 0) + (arrivals.count(u) ? 1 : 0) == 1, "written once", u, 0);
         if (!arrivals.count(u)) continue;
         check(arrivals[u] == counts[u] && counts[u] > 1, "arrivals", arrivals[u], counts[u]);
-        const int f = sh.of(first_of[u]);
+        const int f = first_wg[u];
         for (int k = 0; k < counts[u]; ++k)
             check(parts[u].count({f + k, k == 0}) == 1, "a part where it is looked for", u, k);
         check((int)parts[u].size() == counts[u], "parts", (long long)parts[u].size(), counts[u]);

@@ -713,18 +713,26 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     __syncthreads();
 
     // join the parts in LDS, run by run of one unit's (lane i: part i), a pair of
-    // outputs per thread
+    // outputs per thread; several runs at a time, of as many waves each
     const int pairs = G * D / 2;
     const int own_unit = lane < NE ? unit[lane] : -1;
-    unsigned left = (unsigned)__ballot(own_unit >= 0);
-    while (left) {
-        const int e = __builtin_ctz(left);
-        const int u = __builtin_amdgcn_readlane(own_unit, e);
-        const unsigned run = (unsigned)__ballot(own_unit == u);
-        left &= ~run;
+    const auto for_runs = [&](auto &&f) {
+        int k = 0;
+        for (unsigned left = (unsigned)__ballot(own_unit >= 0); left; ++k) {
+            const int u = __builtin_amdgcn_readlane(own_unit, __builtin_ctz(left));
+            const unsigned run = (unsigned)__ballot(own_unit == u);
+            left &= ~run;
+            f(k, u, run);
+        }
+        return k;
+    };
+    const int runs = for_runs([](int, int, unsigned) {});
+    const int team = runs >= 8 ? 1 : runs >= 4 ? 2 : runs >= 2 ? 4 : 8;   // waves per run
+    for_runs([&](int k, int u, unsigned run) {
+        if ((k & (kAttnWaves / team - 1)) != wave / team) return;
+        const int e = __builtin_ctz(run), nr = __builtin_popcount(run);
         const bool whole = u != sent0 && u != sent1;
-        const int nr = __builtin_popcount(run);
-        for (int i = tid; i < pairs; i += kAttnThreads) {
+        for (int i = (wave & (team - 1)) * 64 + lane; i < pairs; i += team * 64) {
             const int h = i / (D / 2), dd = 2 * (i % (D / 2));
             Joined a;
             // (each wave has one part of a unit at most)
@@ -743,7 +751,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 if (dd == 0) st_dev_f2(w + D, a.m, a.l);
             }
         }
-    }
+    });
     if (sent0 < 0 && sent1 < 0) return;
 
     // arrive with what was handed on; the last to arrive joins a unit's parts

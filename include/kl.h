@@ -339,6 +339,7 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  *              (batch * n_kv_heads * max_pages * page_size <= 2^35)
  *   q, out     n_heads heads; n_heads a multiple of n_kv_heads, at most 16
  *              times as many
+ *              (out overlaps neither q nor the pool)
  *   scale      finite
  *   lse        dev fp32 [batch][n_heads] or NULL: max_j + ln sum_j of scale q.k
  *              (what joins this result with one over other positions)

@@ -11,7 +11,7 @@
 namespace kl {
 
 // out_h = sum_j p_j v_j / sum_j p_j, p_j = 2^(s_j - m), s_j = (scale log2 e) q_h . k_j,
-// m at least the largest s_j less 8, over the attended positions j.
+// m the largest s_j and up to 8 more, over the attended positions j.
 //
 // Split-K flash decoding over pages, bound by HBM: at 262144 positions of 8 KV
 // heads 6.1 TB/s bf16, 5.7 e4m3 and 5.0 at head dimension 64 (a read stream:
@@ -51,8 +51,9 @@ namespace kl {
 // bits that bf16 cannot hold, and the probabilities, are taken as several bf16
 // terms: three are all 24 bits of a float; two where the queries are bf16 and the
 // output has 16 bits (a weight is off by 2^-16 of itself at most, a 32nd of a
-// half-step of fp16).  Softmax and sums are fp32; the maximum moves only when a
-// score passes it by 2^8, so the loop has no cross-lane step.
+// half-step of fp16).  Softmax and sums are fp32; m is set 8 above the largest
+// score (in log2 units) and moves only when a score passes it, so the loop has no
+// cross-lane step and no weight is above 1.
 
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -441,7 +442,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     // scores are c S^T in log2 units, c > 0: a negative scale's sign is in the
     // queries, as is a zero scale
     const float c = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.4426950408889634f;
-    float m = -INFINITY, l = 0.f;   // the column's maximum (log2 units), this lane's share of its sum
+    float m = -INFINITY, l = 0.f;   // the column's m (log2 units), this lane's share of its sum
     f32x4 o[EV];                    // O^T: element EV (4 k4 + i) + e of head n in o[e][i]
     auto clear = [&]() {
         m = -INFINITY;
@@ -525,8 +526,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 #pragma unroll
             for (int v = 0; v < NV; ++v) mx = fmaxf(mx, s[sb][v]);
         mx *= c;
-        if (__any(mx > m + 8.f)) {
-            const float mn = fmaxf(m, over_copies<C>(max_16_32(mx), MaxOp()));
+        if (__any(mx > m)) {
+            const float mn = fmaxf(m, over_copies<C>(max_16_32(mx), MaxOp()) + 8.f);
             const float al = __builtin_amdgcn_exp2f(m - mn);
             l *= al;
 #pragma unroll

@@ -282,6 +282,26 @@ def test_attention_rising_and_falling_scores():
         check_attention(out, lse, want)
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+def test_attention_of_large_and_tiny_values(cache):
+    # sums stay below the largest value where the weights do not pass 1, also
+    # while scores rise; tiny values keep their precision
+    d, n, page = 128, 300, 16
+    for mag in (1.2e36, 1e-30):
+        pool = make_pool(1, 20, 1, page, d, cache, gen(3))
+        k = torch.zeros(n, 1, d)
+        k[:, 0, 0] = torch.arange(n).float() * 0.125
+        v = (torch.rand(n, 1, d, generator=gen(9)) + 0.5) * mag
+        table = make_table([n], page, 20, gen(4))
+        pos = torch.arange(n, dtype=torch.int32).cuda()
+        pool.append(0, table.cuda(), pos, k.cuda(), v.cuda(), seq=torch.zeros_like(pos))
+        q = torch.zeros(1, 2, d)
+        q[:, 0, 0], q[:, 1, 0] = 10.0, -4.0
+        want = attention64(values(pool, "k"), values(pool, "v"), table, [n], q, page, d ** -0.5)
+        out, lse = run_attention(pool, table, [n], q, page)
+        check_attention(out, lse, want)
+
+
 def garbage(pool, used):
     """Everything that no attended position uses: NaN, infinities, and scale bytes of all kinds."""
     for name in ("k", "v"):

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         return checked(reinterpret_cast<const KL_KARG int32_t *>(
             reinterpret_cast<uint64_t>(p.lengths))[b]);
     };
-    // The workgroup's share [X0, X1): of one unit (unit_shares), or an equal
+    // The workgroup's share [X0, X1): of one unit (unit_groups), or an equal
     // share, with a workgroup for every kAttnWaves tiles.  Units of several
     // workgroups: the one that the share begins inside of, and the one that
     // begins in the share and goes on behind it; their numbers of workgroups,
@@ -236,11 +236,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     if (few && B * nkv <= groups) {
         const int equal = uni(equal_rounds(T, groups, kAttnWaves));
         const int most = uni((int)wave_max((float)tiles_own));   // (exact where it matters: below 2^24)
-        for (int r = equal; r <= equal + kUnitRounds && !by_unit; ++r) {
-            const int own = unit_groups(tiles_own, r, kAttnWaves), to = wave_scan(own);
-            by_unit = unit_shares(__builtin_amdgcn_readlane(to, B - 1) * nkv, groups, most, r, equal,
-                                  kAttnWaves);
-            if (!by_unit) continue;
+        const bool half = half_shares(most, equal, kAttnWaves);
+        for (int per = half ? kHalfShare : equal * kAttnWaves;; per = equal * kAttnWaves) {
+            const int own = unit_groups(tiles_own, per), to = wave_scan(own);
+            by_unit = __builtin_amdgcn_readlane(to, B - 1) * nkv <= groups;
+            if (!by_unit && per == kHalfShare) continue;
+            if (!by_unit) break;
             if (wg >= __builtin_amdgcn_readlane(to, B - 1) * nkv) return;
             const int b = __popcll(__ballot(lane < B && to * nkv <= wg));
             const int n = __builtin_amdgcn_readlane(own, b), nt = __builtin_amdgcn_readlane(tiles_own, b);
@@ -255,6 +256,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             }
             if (j > 0) sent0 = b * nkv + g, from0 = wg - j, count0 = n;
             else if (n > 1) sent1 = b * nkv + g, count1 = n;
+            break;
         }
     }
     Shares sh(1, 1);
@@ -837,13 +839,11 @@ static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
             done.fetch_or(bit, std::memory_order_relaxed);
         }
     }
-    // at most a workgroup for every kAttnWaves tiles that the table has room for
-    const long long tiles = (((long long)p.t.max_pages << p.c.page_log2) + paged_tile(D, F8 ? 1 : 2) - 1) /
-                            paged_tile(D, F8 ? 1 : 2) * p.t.batch * p.c.nkv;
-    // (or for every unit)
-    const int grid = (int)std::min<long long>(
-        std::max<long long>((tiles + kAttnWaves - 1) / kAttnWaves, (long long)p.t.batch * p.c.nkv),
-        kPagedGroups);
+    // for as many tiles as the table has room for
+    constexpr int NK = paged_tile(D, F8 ? 1 : 2);
+    const long long most = (((long long)p.t.max_pages << p.c.page_log2) + NK - 1) / NK;
+    const long long units = (long long)p.t.batch * p.c.nkv;
+    const int grid = (int)std::min<long long>(wanted_groups(most, units, kAttnWaves), kPagedGroups);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(kAttnThreads), lds, stream, p);
     return hipGetLastError();
 }

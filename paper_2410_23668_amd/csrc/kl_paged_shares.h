@@ -44,24 +44,38 @@ struct Shares {
 };
 
 // Where it can be had at no cost, a workgroup has tiles of one unit only: each
-// unit gets whole workgroups, as many as make shares of at most r rounds (a
-// round is a tile for each of the workgroup's waves, about 2 us).  A workgroup
-// then hands on one part and not two, and units of r rounds at most need no
-// part in memory at all, which is worth about 4 us: for those r may be up to
-// kUnitRounds above what equal shares have.
-constexpr int kUnitRounds = 2;
+// unit gets whole workgroups, as many as make shares of at most 'per' tiles.  A
+// workgroup then hands on one part and not two, and a unit of one workgroup
+// needs no part in memory at all, which is worth about 4 us.
+//   per = equal rounds   the rounds (a tile for each of the workgroup's waves)
+//                        that an equal share has, in tiles;
+//   per = kHalfShare     half a round, where no unit fits into one workgroup
+//                        anyway: twice the workgroups, and less for each to
+//                        load and join, as long as a unit's parts are read in
+//                        one go (kHalfParts of them).
+// 32 heads on 8 of 128, bf16, one sequence, half rounds against whole: 1024
+// positions 10.9 us against 11.7, 2048 11.7 against 12.3; 4096, 32 parts, 14.8
+// against 13.6.  Against a unit of more rounds in one workgroup: 512 positions
+// 10.5 against 11.5 in two, 768 10.7 against 11.6 in three (but 384, a round
+// and a half, 10.5 against 10.3).
+constexpr int kHalfShare = 4, kHalfParts = 16;
 KL_HD inline int equal_rounds(int T, int groups, int waves) {
     const int each = (T + groups - 1) / groups;
     return (each + waves - 1) / waves;
 }
 // workgroups of a unit of nt tiles
-KL_HD inline int unit_groups(int nt, int r, int waves) {
-    const int rounds = (nt + waves - 1) / waves;
-    return r == 1 ? rounds : (rounds + r - 1) / r;
+KL_HD inline int unit_groups(int nt, int per) { return (nt + per - 1) / per; }
+// whether half rounds are tried, for units of at most 'most' tiles
+KL_HD inline bool half_shares(int most, int equal, int waves) {
+    return most > equal * waves && most <= kHalfParts * kHalfShare;
 }
-// whether 'need' workgroups so, for units of at most 'most' tiles, are taken
-KL_HD inline bool unit_shares(int need, int groups, int most, int r, int equal, int waves) {
-    return need <= groups && (r == equal || most <= r * waves);
+// Workgroups to launch for units of up to 'most' tiles each: one for every
+// round, one for every half round that may be taken, and one for every unit.
+KL_HD inline long long wanted_groups(long long most, long long units, int waves) {
+    const long long round = (most * units + waves - 1) / waves;
+    const long long capped = most < kHalfParts * kHalfShare ? most : kHalfParts * kHalfShare;
+    const long long half = (capped + kHalfShare - 1) / kHalfShare * units;
+    return round > half ? round : half;   // (half >= units: most >= 1)
 }
 
 }  // namespace kl

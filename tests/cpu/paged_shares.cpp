@@ -44,16 +44,22 @@ void walk(const std::vector<int> &lengths, int nkv, int window, int NK, int grid
     const int units = B * nkv, equal = equal_rounds(T, grid, kWaves);
     bool by_unit = false;
     std::vector<int> unit_wg, part_wg, groups_of(units);   // by workgroup; by unit
-    for (int r = equal; may_by_unit && r <= equal + kUnitRounds && !by_unit; ++r) {
+    const bool half = half_shares(most, equal, kWaves);
+    for (int per = half ? kHalfShare : equal * kWaves; may_by_unit && units <= grid; per = equal * kWaves) {
         int need = 0;
-        for (int u = 0; u < units; ++u) need += groups_of[u] = unit_groups(nt[u], r, kWaves);
-        by_unit = unit_shares(need, grid, most, r, equal, kWaves);
+        for (int u = 0; u < units; ++u) {
+            need += groups_of[u] = unit_groups(nt[u], per);
+            check(per != kHalfShare || groups_of[u] <= kHalfParts, "parts", u, groups_of[u]);
+        }
+        by_unit = need <= grid;
+        if (!by_unit && per == kHalfShare) continue;
         if (by_unit)
             for (int u = 0; u < units; ++u)
                 for (int j = 0; j < groups_of[u]; ++j) {
                     unit_wg.push_back(u);
                     part_wg.push_back(j);
                 }
+        break;
     }
     const int want = (T + kWaves - 1) / kWaves < grid ? (T + kWaves - 1) / kWaves : grid;
     const Shares sh(T, want);
@@ -168,6 +174,8 @@ int main() {
                 check(s.of(a) == i && s.of(b - 1) == i, "of", T, i);
             }
         }
+    check(wanted_groups(1, 7, 8) == 7 && wanted_groups(3, 8, 8) == 8 && wanted_groups(64, 1, 8) == 16 &&
+              wanted_groups(65, 1, 8) == 16 && wanted_groups(1000, 2, 8) == 250, "launched", 0, 0);
     std::srand(7);
     const int grids[] = {1, 2, 5, 64, 256};
     for (int it = 0; it < 3000; ++it) {

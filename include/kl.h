@@ -350,8 +350,9 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  *              workspace each.
  * Scores, softmax and sums are held in 32 bits, and a sequence's result does
  * not depend on timing (parts are joined in a fixed order).  Slots outside the
- * attended positions do not affect the result, whatever they hold; a NaN or
- * infinity in an attended slot makes the head's output non-finite.
+ * attended positions do not affect the result, whatever they hold; with a NaN or
+ * an infinity in an attended slot the outputs of its KV head's query heads may
+ * be NaN.  A score that overflows downwards has no weight.
  * Device error bits: KL_DEVERR_POSITION for a length outside [0, max_pages *
  * page_size], KL_DEVERR_PAGE for a bad table entry of an attended position;
  * the sequence's output row and lse are then NaN. */
@@ -370,7 +371,7 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
  * dispatches).
  *   cache    of the model's n_layers, n_kv_heads, head_dim and device
  *   table    batch >= the step's; positions are < max_pages * page_size and
- *            < max_seq
+ *            < max_seq (batch * n_kv_heads * the smaller of the two <= 2^35)
  * The other arguments, results and errors as for kl_decode_step; a bad table
  * entry up to the position's sets KL_DEVERR_PAGE, and its sequence is skipped
  * as one with a bad position (KL_DEVERR_POSITION).  KL_ERR_UNSUPPORTED for a

@@ -10,8 +10,9 @@
 
 namespace kl {
 
-// out_h = sum_j p_j v_j / sum_j p_j, p_j = 2^(s_j - m), s_j = (scale log2 e) q_h . k_j,
-// m the largest s_j and up to 8 more, over the attended positions j.
+// out_h = sum_j p_j v_j / sum_j p_j, p_j = 2^(c (s_j - m) - 8), s_j = q_h . k_j,
+// c = scale log2 e, m the largest s_j of the attended positions j, or up to 8 / c
+// less.
 //
 // Split-K flash decoding over pages, bound by HBM: at 262144 positions of 8 KV
 // heads 6.1 TB/s bf16, 5.7 e4m3 and 5.0 at head dimension 64 (a read stream:
@@ -25,7 +26,7 @@ namespace kl {
 // to its eight waves, so that lengths of any kind load every wave alike (few
 // units: kl_paged_shares.h).  A wave goes through its tiles with a running
 // maximum and sum; a unit that lies inside its share it writes out, of a unit
-// cut by the share's ends it leaves its part (maximum, sum, unnormalised output)
+// cut by the share's ends it leaves its part (m, sum, unnormalised output)
 // in LDS.  The workgroup joins the parts there; what is part of a unit of several
 // workgroups goes to the workspace, and the last of them to arrive (a counter
 // per unit) joins all in workgroup order.
@@ -51,9 +52,10 @@ namespace kl {
 // bits that bf16 cannot hold, and the probabilities, are taken as several bf16
 // terms: three are all 24 bits of a float; two where the queries are bf16 and the
 // output has 16 bits (a weight is off by 2^-16 of itself at most, a 32nd of a
-// half-step of fp16).  Softmax and sums are fp32; m is set 8 above the largest
-// score (in log2 units) and moves only when a score passes it, so the loop has no
-// cross-lane step and no weight is above 1.
+// half-step of fp16).  Softmax and sums are fp32; m moves only when a score is more
+// than 8 / c above it, so the loop has no cross-lane step and no weight is above
+// 1.  It is taken from the scores before they are multiplied: c s - m would carry
+// the rounding of a product, more than 8 where scores are above 2^27.
 
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -85,26 +87,29 @@ __device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
     }
 }
 
-// Two neighbouring outputs of a head, unnormalised, with their maximum (log2
-// units) and sum.
-struct Joined { float o0 = 0.f, o1 = 0.f, m = -INFINITY, l = 0.f; };
-// Adds the first n (at most NB) of the parts that get(j, outputs, (maximum,
-// sum)) reads, all of them at once.
+// m where no score has been seen: below every one, and finite, so that there is
+// no difference of infinities.
+constexpr float kNoScore = -3.402823466e38f;
+
+// Two neighbouring outputs of a head, unnormalised, with their m and sum.
+struct Joined { float o0 = 0.f, o1 = 0.f, m = kNoScore, l = 0.f; };
+// Adds the first n (at most NB) of the parts that get(j, outputs, (m, sum))
+// reads, all of them at once.
 template <int NB, class Get>
-__device__ __forceinline__ void join_parts(int n, Joined &a, Get &&get) {
+__device__ __forceinline__ void join_parts(int n, float c, Joined &a, Get &&get) {
     f32x2 o[NB], ml[NB];
     float mn = a.m;
 #pragma unroll
     for (int j = 0; j < NB; ++j) get(j, o[j], ml[j]);
 #pragma unroll
     for (int j = 0; j < NB; ++j) mn = j < n ? fmaxf(mn, ml[j][0]) : mn;
-    const float al = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - mn);   // (none yet: 0)
+    const float al = __builtin_amdgcn_exp2f((a.m - mn) * c);
     a.l *= al;
     a.o0 *= al;
     a.o1 *= al;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        const float w = __builtin_amdgcn_exp2f(ml[j][0] - mn);
+        const float w = __builtin_amdgcn_exp2f((ml[j][0] - mn) * c);
         a.l = j < n ? fmaf(ml[j][1], w, a.l) : a.l;
         a.o0 = j < n ? fmaf(o[j][0], w, a.o0) : a.o0;
         a.o1 = j < n ? fmaf(o[j][1], w, a.o1) : a.o1;
@@ -417,9 +422,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     };
 
     const int out_bytes = p.out_type == KL_DTYPE_FP32 ? 4 : 2;
-    // head h of the group, of maximum M (log2 units) and sum L
+    // scores are c S^T in log2 units, c > 0: a negative scale's sign is in the
+    // queries, as is a zero scale
+    const float abs_scale = p.scale == 0.f ? 1.f : fabsf(p.scale), c = abs_scale * 1.4426950408889634f;
+    // head h of the group, of m M and sum L
     auto write_lse = [&](int b, int g, int h, float M, float L) {
-        p.lse[(long long)b * p.nq + g * G + h] = (M + __log2f(L)) * 0.69314718055994531f;
+        p.lse[(long long)b * p.nq + g * G + h] =
+            fmaf(M, abs_scale, (8.f + __log2f(L)) * 0.69314718055994531f);
     };
     // its elements dd and dd + 1
     auto write_pair = [&](int b, int g, int h, int dd, const Joined &a) {
@@ -441,13 +450,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         if (p.lse && dd == 0) write_lse(b, g, h, a.m, a.l);
     };
 
-    // scores are c S^T in log2 units, c > 0: a negative scale's sign is in the
-    // queries, as is a zero scale
-    const float c = p.scale == 0.f ? 1.f : fabsf(p.scale) * 1.4426950408889634f;
-    float m = -INFINITY, l = 0.f;   // the column's m (log2 units), this lane's share of its sum
+    float m = kNoScore, l = 0.f;    // the column's m, this lane's share of its sum
     f32x4 o[EV];                    // O^T: element EV (4 k4 + i) + e of head n in o[e][i]
     auto clear = [&]() {
-        m = -INFINITY;
+        m = kNoScore;
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < EV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -527,10 +533,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         for (int sb = 0; sb < NS; ++sb)
 #pragma unroll
             for (int v = 0; v < NV; ++v) mx = fmaxf(mx, s[sb][v]);
-        mx *= c;
-        if (__any(mx > m)) {
-            const float mn = fmaxf(m, over_copies<C>(max_16_32(mx), MaxOp()) + 8.f);
-            const float al = __builtin_amdgcn_exp2f(m - mn);
+        if (__any((mx - m) * c > 8.f)) {
+            const float mn = fmaxf(m, over_copies<C>(max_16_32(mx), MaxOp()));
+            const float al = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= al;
 #pragma unroll
             for (int i = 0; i < EV; ++i) o[i] *= al;
@@ -541,7 +546,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             float pr[NV];
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                pr[v] = __builtin_amdgcn_exp2f(fmaf(s[sb][v], c, -m));
+                pr[v] = __builtin_amdgcn_exp2f(fmaf(s[sb][v] - m, c, -8.f));
                 l += pr[v];
                 if constexpr (F8) pr[v] *= pow2_of(scale_byte(vsr[sb], v));
             }
@@ -631,6 +636,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             }
             if (a.len == 0) {   // (nothing attended: what was computed is void)
                 clear();
+                m = -INFINITY;
                 L = 1.f;
             }
             // into LDS: a unit's part, or a whole unit on its way out (in the
@@ -749,7 +755,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             Joined a;
             // (each wave has one part of a unit at most)
             unsigned r = run;
-            join_parts<kAttnWaves>(nr, a, [&](int, f32x2 &o, f32x2 &ml) {
+            join_parts<kAttnWaves>(nr, c, a, [&](int, f32x2 &o, f32x2 &ml) {
                 const float *w = part + ((r ? __builtin_ctz(r) : e) * G + h) * WD;
                 r &= r - 1;
                 o = *reinterpret_cast<const f32x2 *>(w + dd);
@@ -795,7 +801,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             Joined a;
             if (sub < S && i < pairs) {
                 for (int k0 = sub; k0 < nw; k0 += S * NB)
-                    join_parts<NB>((nw - k0 + S - 1) / S, a, [&](int j, f32x2 &o, f32x2 &ml) {
+                    join_parts<NB>((nw - k0 + S - 1) / S, c, a, [&](int j, f32x2 &o, f32x2 &ml) {
                         const int k = min(k0 + j * S, nw - 1);
                         const float *w = p.parts + ((size_t)((f + k) * 2 + (k == 0)) * G + h) * WD;
                         o = ld_dev_f2(w + dd);
@@ -808,7 +814,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 __syncthreads();
                 if (sub == 0) {
                     for (int k = 1; k < min(S, nw); ++k)
-                        join_parts<1>(1, a, [&](int, f32x2 &o, f32x2 &ml) {
+                        join_parts<1>(1, c, a, [&](int, f32x2 &o, f32x2 &ml) {
                             const f32x4 v = x[tid + k * pairs];
                             o = f32x2{v[0], v[1]};
                             ml = f32x2{v[2], v[3]};

@@ -302,6 +302,77 @@ def test_attention_of_large_and_tiny_values(cache):
         check_attention(out, lse, want)
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("io", [BF16, FP32])
+@pytest.mark.parametrize("key,query,scale", [(2.0 ** 20, 2.0 ** 20, 0.125), (2.0 ** 20, 2.0 ** 20, -0.125),
+                                             (2.0 ** 100, 2.0 ** 26, 1.0)])
+def test_attention_of_scores_far_apart(cache, io, key, query, scale):
+    # scores are multiples of 2^37 (or 2^126): the largest have all the weight, shared
+    # equally, whatever the rounding of scores in log2 units
+    d, page, lengths = 64, 16, [1, 40, 1500, 5000]
+    pool = make_pool(1, 450, 2, page, d, cache, gen(3))
+    table = make_table(lengths, page, 450, gen(4))
+    out_of = torch.empty(4, 6, d, dtype=torch.float64)
+    tol, lse_of = torch.empty_like(out_of), torch.empty(4, 6, dtype=torch.float64)
+    rows = []
+    for b, n in enumerate(lengths):
+        m = torch.randint(-3, 2, (n, 2), generator=gen(b)).float()
+        m[n // 2:] += 1   # (the maximum of the first half is passed)
+        k = torch.zeros(n, 2, d)
+        k[:, :, 0] = m * key
+        v = torch.randn(n, 2, d, generator=gen(20 + b))
+        pos = torch.arange(n, dtype=torch.int32)
+        seq = torch.full_like(pos, b)
+        pool.append(0, table.cuda(), pos.cuda(), k.cuda(), v.cuda(), seq=seq.cuda())
+        rows.append(m)
+    V = values(pool, "v")
+    for b, n in enumerate(lengths):
+        pg, off = table[b].long()[torch.arange(n) // page], torch.arange(n) % page
+        for h in range(6):
+            x = rows[b][:, h // 3] * (1 if scale > 0 else -1)
+            top = x == x.max()
+            v = V[0, pg, h // 3, off][top]
+            out_of[b, h] = v.mean(0)
+            tol[b, h] = 2.0 ** -24 * (32 + 8 * math.sqrt(n)) * v.abs().mean(0)
+            lse_of[b, h] = float(x.max()) * key * query * abs(scale) + math.log(int(top.sum()))
+    ltol = 2.0 ** -23 * lse_of.abs() + 2.0 ** -24 * (32 + 8 * math.sqrt(5000))
+    q = torch.zeros(4, 6, d)
+    q[:, :, 0] = query
+    out, lse = run_attention(pool, table, lengths, q.to(io), page, scale=scale)
+    check_attention(out, lse, (out_of, lse_of, tol, ltol))
+
+
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("io", [BF16, FP32])
+def test_attention_of_scores_that_overflow(cache, io):
+    # a score below every number (its sum of products overflows) has no weight: at the
+    # sequence's start, for whole tiles and workgroups, in between, or everywhere (NaN)
+    d, page, n = 128, 16, 3000
+    for where in (slice(0, 2000), slice(1, None, 2), slice(0, 2999), slice(10, None), slice(0, None)):
+        pool = make_pool(1, 200, 1, page, d, cache, gen(3))
+        table = make_table([n], page, 200, gen(4))
+        k = torch.zeros(n, 1, d)
+        k[where, 0, 0] = -2.0 ** 100
+        v = torch.randn(n, 1, d, generator=gen(9))
+        pos = torch.arange(n, dtype=torch.int32).cuda()
+        pool.append(0, table.cuda(), pos, k.cuda(), v.cuda(), seq=torch.zeros_like(pos))
+        q = torch.zeros(1, 2, d)
+        q[:, 0, 0] = 2.0 ** 100   # (the other head: all scores 0)
+        out, lse = run_attention(pool, table, [n], q.to(io), page)
+        V = values(pool, "v")[0, table[0].long()[torch.arange(n) // page], 0, torch.arange(n) % page]
+        some = torch.ones(n, dtype=torch.bool)
+        some[where] = False
+        for h, left in ((0, some), (1, torch.ones_like(some))):
+            if not bool(left.any()):
+                assert bool(torch.isnan(out[0, h]).all()) and float(lse[0, h]) == -math.inf
+                continue
+            x = V[left]
+            tol = 2.0 ** -24 * (32 + 8 * math.sqrt(n)) * x.abs().mean(0)
+            want = (x.mean(0), torch.tensor(math.log(len(x)), dtype=torch.float64), tol,
+                    torch.tensor(2.0 ** -24 * (32 + 8 * math.sqrt(n) + 16)))
+            check_attention(out[0, h], lse[0, h], want, f"{where}, head {h}")
+
+
 def garbage(pool, used):
     """Everything that no attended position uses: NaN, infinities, and scale bytes of all kinds."""
     for name in ("k", "v"):

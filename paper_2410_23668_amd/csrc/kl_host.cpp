@@ -817,6 +817,9 @@ kl_status kl_decode_step_paged(kl_state *st, const int32_t *token_ids, const int
     stt = check_step_args(st, token_ids, positions, batch, &kv, logits_out, hidden_out,
                           KL_MODE_PER_OP);
     if (stt != KL_OK) return stt;
+    // (as kl_paged_attention's: its tiles are counted in 32 bits)
+    if ((int64_t)batch * c.n_kv_heads * (((int64_t)kv.capacity + 31) / 32) > (1 << 30))
+        return fail(KL_ERR_UNSUPPORTED, "%s: batch * n_kv_heads * positions above 2^35", who);
 
     StepParams P = step_params(*st, st->scratch, plan_scratch(*st, c.max_batch, false), token_ids,
                                rows, batch, &kv, logits_out, hidden_out);

@@ -194,3 +194,16 @@ def test_refusals():
     assert st == kb.KL_ERR_UNSUPPORTED
     assert kb.lib().kl_decode_step_paged(None, 16, 16, 1, pool.c, pool._table(table), 16, None,
                                          None) == kb.KL_ERR_INVALID_ARGUMENT
+
+
+def test_room_for_more_tiles_than_32_bits_count_is_refused():
+    cfg = dict(TINY, n_layers=1, n_heads=16, n_kv_heads=16)
+    case = Case(cfg, 2, 64, [3, 4], seed=43, max_batch=4096, max_seq=2 ** 20)
+    pool = PagedKvCache(cfg, 2, 4096)
+    B = 4096
+    table = torch.zeros(B, 256, dtype=torch.int32, device="cuda")
+    tok, pos = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2))
+    lg = torch.empty(B, cfg["vocab"], device="cuda")
+    with pytest.raises(kb.KlError) as e:
+        case.model.step_paged(tok, pos, pool, table, lg)
+    assert e.value.status == kb.KL_ERR_UNSUPPORTED and "2^35" in str(e.value)

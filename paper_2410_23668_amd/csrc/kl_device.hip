@@ -179,8 +179,8 @@ hipError_t launch_step(const StepParams &p, int first_layer, int last_layer, int
     return hipGetLastError();
 }
 
-hipError_t add_step_node(hipGraph_t g, hipGraphNode_t *node, const hipGraphNode_t *dep,
-                         const StepParams &p, int first_layer, int last_layer, int phases,
+hipError_t add_step_node(hipGraph_t g, hipGraphNode_t *node, const hipGraphNode_t *deps,
+                         size_t n_deps, const StepParams &p, int first_layer, int last_layer, int phases,
                          bool cooperative, int lds_bytes) {
     const StepKernel k = step_kernel_for(p.d, p.group, p.batched != 0);
     if (!k) return hipErrorInvalidValue;
@@ -192,11 +192,26 @@ hipError_t add_step_node(hipGraph_t g, hipGraphNode_t *node, const hipGraphNode_
     kp.blockDim = dim3(kThreads);
     kp.sharedMemBytes = (unsigned)lds_bytes;
     kp.kernelParams = args;
-    hipError_t e = hipGraphAddKernelNode(node, g, dep, dep ? 1 : 0, &kp);
+    hipError_t e = hipGraphAddKernelNode(node, g, deps, n_deps, &kp);
     if (e != hipSuccess || !cooperative) return e;
     hipKernelNodeAttrValue v{};
     v.cooperative = 1;
     return hipGraphKernelNodeSetAttribute(*node, hipKernelNodeAttributeCooperative, &v);
+}
+
+hipError_t capture_step(const StepParams &p, int first_layer, int last_layer, int phases,
+                        bool cooperative, int lds_bytes, hipStream_t stream) {
+    hipStreamCaptureStatus status;
+    unsigned long long id;
+    hipGraph_t g;
+    const hipGraphNode_t *deps;
+    size_t n;
+    hipError_t e = hipStreamGetCaptureInfo_v2(stream, &status, &id, &g, &deps, &n);
+    if (e != hipSuccess) return e;
+    hipGraphNode_t node;
+    e = add_step_node(g, &node, deps, n, p, first_layer, last_layer, phases, cooperative, lds_bytes);
+    if (e != hipSuccess) return e;
+    return hipStreamUpdateCaptureDependencies(stream, &node, 1, hipStreamSetCaptureDependencies);
 }
 
 hipError_t launch_pack_rows(uint16_t *dst, int n_rg, int kt, int K, int ld, const int32_t *rowmap,

@@ -676,14 +676,14 @@ static kl_status launch_layer_graph(kl_state *st, const StepParams &P, hipStream
         const bool bat = P.batched != 0;
         const int lds = st->lds.bytes;
         hipGraphNode_t prev = nullptr, node = nullptr;
-        HIP_TRY(add_step_node(st->graph, &node, nullptr, P, 0, 0, kPhEmbed, false, lds));
+        HIP_TRY(add_step_node(st->graph, &node, nullptr, 0, P, 0, 0, kPhEmbed, false, lds));
         for (int l = 0; l < P.L; ++l) {
             prev = node;
-            HIP_TRY(add_step_node(st->graph, &node, &prev, P, l, l + 1, kPhLayer,
+            HIP_TRY(add_step_node(st->graph, &node, &prev, 1, P, l, l + 1, kPhLayer,
                                   launch_waits_inside(kPhLayer, bat), lds));
         }
         prev = node;
-        HIP_TRY(add_step_node(st->graph, &node, &prev, P, 0, 0, kPhHead,
+        HIP_TRY(add_step_node(st->graph, &node, &prev, 1, P, 0, 0, kPhHead,
                               launch_waits_inside(kPhHead, bat), lds));
         HIP_TRY(hipGraphInstantiate(&st->graph_exec, st->graph, nullptr, nullptr, 0));
         for (int i = 0; i < 10; ++i) st->graph_key[i] = key[i];
@@ -861,8 +861,11 @@ kl_status kl_decode_step_paged(kl_state *st, const int32_t *token_ids, const int
     A.error = st->err;
 
     const int lds = st->lds.bytes;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing(s, &capture));
+    const auto launch = capture == hipStreamCaptureStatusActive ? capture_step : launch_step;
     const auto phase = [&](int l0, int l1, int ph) {
-        return launch_step(P, l0, l1, ph, launch_waits_inside(ph, true), lds, s);
+        return launch(P, l0, l1, ph, launch_waits_inside(ph, true), lds, s);
     };
     // the phases between two layers' attentions in as few launches as the step
     // kernel's order of phases allows

@@ -125,11 +125,16 @@ StepKernel step_kernel_d128_batched(int group);
 
 hipError_t launch_step(const StepParams &p, int first_layer, int last_layer, int phases,
                        bool cooperative, int lds_bytes, hipStream_t stream);
-// Adds the same launch as a kernel node of graph g after 'dep' (null: none);
+// Adds the same launch as a kernel node of graph g after the nodes 'deps';
 // cooperative nodes carry the graph's cooperative attribute.
-hipError_t add_step_node(hipGraph_t g, hipGraphNode_t *node, const hipGraphNode_t *dep,
-                         const StepParams &p, int first_layer, int last_layer, int phases,
+hipError_t add_step_node(hipGraph_t g, hipGraphNode_t *node, const hipGraphNode_t *deps,
+                         size_t n_deps, const StepParams &p, int first_layer, int last_layer, int phases,
                          bool cooperative, int lds_bytes);
+// The same into the graph that 'stream' is being captured into (a captured
+// cooperative launch replays as slowly as it launches, about 18 us more than
+// such a node).
+hipError_t capture_step(const StepParams &p, int first_layer, int last_layer, int phases,
+                        bool cooperative, int lds_bytes, hipStream_t stream);
 hipError_t step_kernel_setup(int d, int group, int lds_bytes, int *max_blocks_per_cu);
 
 // The static scratch of kl_decode_step_noalloc: one array per device, of

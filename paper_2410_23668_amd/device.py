@@ -107,7 +107,8 @@ class GpuModel:
     def step_paged(self, tokens: torch.Tensor, positions: torch.Tensor, pool: "PagedKvCache",
                    table: torch.Tensor, logits: torch.Tensor, hidden: torch.Tensor | None = None,
                    stream: torch.cuda.Stream | None = None) -> None:
-        """step() over a paged cache: row b of the table holds sequence b's pages."""
+        """step() over a paged cache: row b of the table holds sequence b's pages.
+        May be captured into a graph."""
         assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
         assert logits.dtype == torch.float32 and logits.is_contiguous()
         B = tokens.numel()

@@ -207,3 +207,41 @@ def test_room_for_more_tiles_than_32_bits_count_is_refused():
     with pytest.raises(kb.KlError) as e:
         case.model.step_paged(tok, pos, pool, table, lg)
     assert e.value.status == kb.KL_ERR_UNSUPPORTED and "2^35" in str(e.value)
+
+
+def test_captured_steps_replay_between_eager_ones():
+    # two graphs of one model (a bf16 and an 8-bit pool), replayed in turn, each replay
+    # checked against the eager step's bits; inputs change in place
+    case = Case(TINY, 6, 256, [0, 5, 63, 64, 130, 31], seed=44, max_batch=8)
+    B, cfg = case.batch, case.cfg
+    tok, pos = torch.from_numpy(case.tokens).cuda(), torch.from_numpy(case.positions).cuda()
+    runs = []
+    for dtype in (BF16, E4M3):
+        pool, table = to_pages(case, 16, dtype)
+        out = [torch.zeros(B, cfg["vocab"], device="cuda"), torch.zeros(B, cfg["hidden"], device="cuda")]
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=stream):
+            case.model.step_paged(tok, pos, pool, table, *out, stream=stream)
+        runs.append((pool, table, out, graph))
+    for i in range(4):
+        for pool, table, out, graph in runs:
+            tokens, at = (case.tokens + 3 * i) % cfg["vocab"], case.positions + i
+            tok.copy_(torch.from_numpy(tokens))
+            pos.copy_(torch.from_numpy(at))
+            for o in out:
+                o.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            got, k = [o.cpu().numpy() for o in out], pool.k.view(torch.uint8).clone()
+            want = paged_step(case, pool, table, tokens, at)   # (writes the same rows again)
+            assert_bit_exact(got, want, f"replay {i}")
+            assert torch.equal(k, pool.k.view(torch.uint8))
+        assert case.model.device_error() == 0
+    # a replay reports and skips what an eager step would
+    pool, table, out, graph = runs[0]
+    table[2, 0] = -1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert case.model.device_error() == kb.KL_DEVERR_PAGE | kb.KL_DEVERR_POSITION
+    assert bool(torch.isnan(out[0][2]).all()) and bool(torch.isfinite(out[0][3]).all())

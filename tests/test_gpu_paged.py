@@ -115,6 +115,35 @@ def test_append_takes_any_strides_and_alignment():
 
 
 @pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_and_values_of_their_own_strides_and_types(cache, d):
+    g = gen(6)
+    kv, page, n = 3, 16, 21
+    table = make_table([n], page, 4, g).cuda()
+    pos = torch.arange(n, dtype=torch.int32).cuda()
+    seq = torch.zeros(n, dtype=torch.int32).cuda()
+    k = torch.randn(4 * n * kv * d, generator=g).to(FP16).cuda().as_strided(
+        (n, kv, d), (3 * kv * d + 8, 2 * d, 1), 8)
+    v = torch.randn(n, kv, d, generator=g).cuda()
+    a, b = (make_pool(1, 4, kv, page, d, cache, gen(1)) for _ in range(2))
+    a.append(0, table, pos, k, v, seq=seq)
+    b.append(0, table, pos, k.float().contiguous(), v, seq=seq)
+    assert same_bits(snapshot(a), snapshot(b))
+    outs = []
+    for ko, vo in ((torch.full((n, kv, d), 7.0, dtype=FP16, device="cuda"),
+                    torch.full((kv, n, d), 7.0, device="cuda").transpose(0, 1)),
+                   (torch.full((n, kv, d), 7.0, dtype=FP16, device="cuda"),
+                    torch.full((n, kv, d), 7.0, device="cuda"))):
+        a.read(0, table, pos, ko, vo, seq=seq)
+        outs.append((ko, vo))
+    for x, y in zip(*outs):
+        assert torch.equal(x, y) and bool((x != 7.0).any())
+    want = [values(a, w)[0, table.cpu()[0].long()[torch.arange(n) // page], :, torch.arange(n) % page]
+            for w in "kv"]
+    assert torch.equal(outs[1][0].cpu(), want[0].to(FP16)) and torch.equal(outs[1][1].cpu(), want[1].float())
+
+
+@pytest.mark.parametrize("cache", [BF16, E4M3])
 def test_bad_rows_are_skipped_and_reported(cache):
     g = gen(6)
     kv, d, page = 2, 64, 8

@@ -352,7 +352,8 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  * not depend on timing (parts are joined in a fixed order).  Slots outside the
  * attended positions do not affect the result, whatever they hold; with a NaN or
  * an infinity in an attended slot the outputs of its KV head's query heads may
- * be NaN.  A score that overflows downwards has no weight.
+ * be NaN.  A score that overflows downwards has no weight, whatever the type of q;
+ * with one that overflows upwards the head's outputs are NaN.
  * Device error bits: KL_DEVERR_POSITION for a length outside [0, max_pages *
  * page_size], KL_DEVERR_PAGE for a bad table entry of an attended position;
  * the sequence's output row and lse are then NaN. */

@@ -71,7 +71,10 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {
     const bf16x2 v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(unsigned, v);
 }
-// NT bf16 terms of 8 floats (x is left as what the terms do not hold)
+// NT bf16 terms of 8 floats (x is left as what the terms do not hold), each cut
+// off towards zero: three hold all 24 bits as rounded ones would, but none has the
+// other sign or is larger than x, so that a product with a term overflows only
+// where the one with x does, and to the same side.
 template <int NT>
 __device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
 #pragma unroll
@@ -79,7 +82,8 @@ __device__ __forceinline__ void split_terms(float (&x)[8], bf16x8 (&t)[NT]) {
         u32x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+            w[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]),
+                                         0x07060302);
             if (i + 1 < NT) {
                 x[2 * j] -= bf_lo(w[j]);
                 x[2 * j + 1] -= bf_hi(w[j]);

@@ -402,6 +402,35 @@ def test_attention_of_scores_that_overflow(cache, io):
             check_attention(out[0, h], lse[0, h], want, f"{where}, head {h}")
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("io,query,key", [(FP32, 2.0 ** 100 * (2 - 2.0 ** -10), -2.0 ** 100),
+                                          (FP32, 3.4e38, -2.0),
+                                          (FP32, 2.0 ** 70 * (1 + 2.0 ** -8 + 2.0 ** -9), -2.0 ** 70),
+                                          (FP16, 2.0 ** 14 * (2 - 2.0 ** -10), -2.0 ** 126)])
+def test_attention_of_scores_that_overflow_whatever_the_query_rounds_to(cache, io, query, key):
+    # products of query and key are below every number, of queries that are no bf16 values:
+    # their bf16 terms must not overflow to both sides, nor where the query itself does not
+    d, page, n = 64, 16, 1200
+    pool = make_pool(1, 80, 1, page, d, cache, gen(3))
+    table = make_table([n], page, 80, gen(4))
+    k = torch.zeros(n, 1, d)
+    k[::2, 0, 0] = key
+    v = torch.randn(n, 1, d, generator=gen(9))
+    pos = torch.arange(n, dtype=torch.int32).cuda()
+    pool.append(0, table.cuda(), pos, k.cuda(), v.cuda(), seq=torch.zeros_like(pos))
+    q = torch.zeros(1, 3, d)
+    q[:, 0, 0], q[:, 1, 0] = query, -query   # (head 1: above every number; head 2: all scores 0)
+    out, lse = run_attention(pool, table, [n], q.to(io), page, scale=1.0)
+    V = values(pool, "v")[0, table[0].long()[torch.arange(n) // page], 0, torch.arange(n) % page]
+    for h, x in ((0, V[1::2]), (2, V)):
+        m = x.shape[0]
+        tol = 2.0 ** -24 * (32 + 8 * math.sqrt(m)) * x.abs().mean(0)
+        want = (x.mean(0), torch.tensor(math.log(m), dtype=torch.float64), tol,
+                torch.tensor(2.0 ** -24 * (32 + 8 * math.sqrt(m) + 16)))
+        check_attention(out[0, h], lse[0, h], want, f"head {h}")
+    assert bool(torch.isnan(out[0, 1]).all())
+
+
 def garbage(pool, used):
     """Everything that no attended position uses: NaN, infinities, and scale bytes of all kinds."""
     for name in ("k", "v"):

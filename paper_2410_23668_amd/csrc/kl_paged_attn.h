@@ -49,15 +49,15 @@ namespace kl {
 // and the copies' outputs are added at the unit's end.
 // e4m3 rows become bf16 (exactly) on the way, keys with their row's scale,
 // values without: theirs goes into the probabilities.  Queries and probabilities
-// are taken as bf16 terms: bf16 queries are one, fp16 ones two; where queries or
-// outputs have 32 bits, both are three, all 24 bits of a float (two for fp16 at
-// 64-byte rows: 50.0 us against 52.1 with three, batch 48, 32 KV heads).  Outputs
-// of 16 bits take two terms of probabilities (a weight is off by 2^-16 of itself
-// at most, a 32nd of a half-step of fp16).  Softmax and sums are fp32; m moves only
-// when a score is more than 8 / c above it, so the loop has no cross-lane step and
-// no weight is above 1.  It is taken from the scores before they are multiplied: c
-// s - m would carry the rounding of a product, more than 8 where scores are above
-// 2^27.
+// are taken as bf16 terms that hold all their bits: bf16 queries are one, fp16 ones
+// two, fp32 ones three, and so are probabilities, whatever the output's type: of
+// two terms a weight would be off by up to 2^-17 of itself, and where values
+// cancel a 16-bit output by many of its own half-steps (two take 1 % less time: 49.7
+// us against 50.2 at batch 48, 32 KV heads of 64, e4m3, fp16).  Softmax and sums are
+// fp32; m moves only when a score is more than 8 / c above it, so the loop has no
+// cross-lane step and no weight is above 1.  It is taken from the scores before they
+// are multiplied: c s - m would carry the rounding of a product, more than 8 where
+// scores are above 2^27.
 
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     constexpr int NC = RB / 64;                 // 16-byte loads of a key row per lane
     constexpr int EV = D / 16, VW = EV * ES / 4;   // value elements, words per lane and position
     constexpr int ST = D / 32;                  // steps of the first product
-    constexpr int PT = QT < 3 ? 2 : 3;          // terms of probabilities (QT: of queries)
+    constexpr int PT = 3;                       // terms of probabilities (QT: of queries)
     constexpr bool kIsBf16 = QT == 1;           // the queries
     constexpr int NV = 8 / C;                   // scores of a block that a lane goes on with
     constexpr int WD = D + 2;                   // floats of a part of one head

@@ -431,6 +431,66 @@ def test_attention_of_scores_that_overflow_whatever_the_query_rounds_to(cache, i
     assert bool(torch.isnan(out[0, 1]).all())
 
 
+def cancelling(pool, group, kv, B, page, d):
+    """Sequences of six positions of which the last five cancel, head by head:
+    keys k0 (the largest score, value 0), kA (value 1) and four times kB, whose
+    values add up to -pA / pB of head e % group in element e."""
+    rows_k, rows_v, qh = [], [], 1 + torch.arange(group).double() / 16
+    step = 2.0 ** -3
+    for b in range(B):
+        a, c = step * (1 + b % 16), step * (2 + (5 * b) % 15)
+        k = torch.zeros(6, kv, d, dtype=torch.float64)
+        k[1, :, 0], k[2:, :, 0] = -a, -c
+        v = torch.zeros(6, kv, d, dtype=torch.float64)
+        v[1] = 1.0
+        left = -torch.exp(qh * (c - a))[torch.arange(d) % group].expand(kv, d)
+        for i in range(2, 6):
+            if pool.k.dtype == BF16:
+                v[i] = left.to(BF16).double()
+            else:
+                codes, s = e4m3_rows(left)
+                v[i] = codes.view(E4M3).float().double() * torch.exp2(s.double() - 127)[..., None]
+            left = left - v[i]
+        rows_k.append(k)
+        rows_v.append(v)
+    table = torch.arange(B, dtype=torch.int32)[:, None].contiguous()
+    pos = torch.arange(6, dtype=torch.int32).repeat(B)
+    seq = torch.arange(B, dtype=torch.int32).repeat_interleave(6)
+    pool.append(0, table.cuda(), pos.cuda(), torch.cat(rows_k).float().cuda(),
+                torch.cat(rows_v).float().cuda(), seq=seq.cuda())
+    q = torch.zeros(B, kv * group, d, dtype=torch.float64)
+    q[:, :, 0] = qh.repeat(kv)
+    return table, q
+
+
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("io", [BF16, FP16, FP32])
+@pytest.mark.parametrize("d,group", [(64, 4), (128, 8), (128, 16)])
+def test_attention_where_values_cancel(cache, io, d, group):
+    # Outputs of a 2^-15th of sum p |v| or less: half a step of any type is far below
+    # what the weights' own rounding leaves.  Scores are exact (one product of 4 and 8
+    # significant bits, at most 4 in magnitude).  A weight: its exponent c (s - m) - 8, below
+    # 16 in magnitude, is rounded by 2^-21 (times ln 2), c by 2^-24 of 5.8 in either of two
+    # roundings, the exponential by 2^-23: 2^-20.5 together; the six products that count are
+    # added in fp32, 2^-23 of sum p |v| each: 2^-20.4.  Together 2^-19.4, of sum p |v|.
+    # (Weights of 16 bits would be off by up to 2^-17.)
+    B, kv, page = 32, 2, 8
+    pool = make_pool(1, B, kv, page, d, cache, gen(5))
+    table, q = cancelling(pool, group, kv, B, page, d)
+    q = q.to(io)
+    want = attention64(values(pool, "k"), values(pool, "v"), table, [6] * B, q, page, 1.0)
+    K, V = values(pool, "k")[0], values(pool, "v")[0]
+    out, lse = run_attention(pool, table, [6] * B, q, page, scale=1.0)
+    mag = torch.zeros_like(want[0])
+    for b in range(B):
+        for h in range(kv * group):
+            p = torch.softmax(K[b, h // group, :6] @ q[b, h].double(), 0)
+            mag[b, h] = p @ V[b, h // group, :6].abs()
+    hit = torch.arange(d)[None] % group == (torch.arange(kv * group) % group)[:, None]
+    assert float((want[0].abs() / mag)[:, hit].max()) < 2.0 ** -15
+    check_attention(out, lse, (want[0], want[1], 2.0 ** -19.4 * mag, want[3]))
+
+
 def garbage(pool, used):
     """Everything that no attended position uses: NaN, infinities, and scale bytes of all kinds."""
     for name in ("k", "v"):

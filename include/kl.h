@@ -348,12 +348,14 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  *              leaves it ready for the next one.  Calls that may run at the
  *              same time (other streams, graphs replayed side by side) need a
  *              workspace each.
- * Scores, softmax and sums are held in 32 bits, and a sequence's result does
- * not depend on timing (parts are joined in a fixed order).  Slots outside the
- * attended positions do not affect the result, whatever they hold; with a NaN or
- * an infinity in an attended slot the outputs of its KV head's query heads may
- * be NaN.  A score that overflows downwards has no weight, whatever the type of q;
- * with one that overflows upwards the head's outputs are NaN.
+ * Keys and values are taken as bf16: those of an e4m3 pool exactly from scale
+ * byte 3 on, below it rounded to multiples of 2^-133.  Scores, softmax and sums
+ * are held in 32 bits, and a sequence's result does not depend on timing (parts
+ * are joined in a fixed order).  Slots outside the attended positions do not
+ * affect the result, whatever they hold; with a NaN or an infinity in an attended
+ * slot the outputs of its KV head's query heads may be NaN.  A score that
+ * overflows downwards has no weight, whatever the type of q; with one that
+ * overflows upwards the head's outputs are NaN.
  * Device error bits: KL_DEVERR_POSITION for a length outside [0, max_pages *
  * page_size], KL_DEVERR_PAGE for a bad table entry of an attended position;
  * the sequence's output row and lse are then NaN. */

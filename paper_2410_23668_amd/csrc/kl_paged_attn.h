@@ -47,17 +47,20 @@ namespace kl {
 // goes on with its own 8 / C of the lane's 8 scores, so that the softmax's
 // vector instructions are spent on a fourth of what 16 columns would need,
 // and the copies' outputs are added at the unit's end.
-// e4m3 rows become bf16 (exactly) on the way, keys with their row's scale,
-// values without: theirs goes into the probabilities.  Queries and probabilities
-// are taken as bf16 terms that hold all their bits: bf16 queries are one, fp16 ones
-// two, fp32 ones three, and so are probabilities, whatever the output's type: of
-// two terms a weight would be off by up to 2^-17 of itself, and where values
-// cancel a 16-bit output by many of its own half-steps (two take 1 % less time: 49.7
-// us against 50.2 at batch 48, 32 KV heads of 64, e4m3, fp16).  Softmax and sums are
-// fp32; m moves only when a score is more than 8 / c above it, so the loop has no
-// cross-lane step and no weight is above 1.  It is taken from the scores before they
-// are multiplied: c s - m would carry the rounding of a product, more than 8 where
-// scores are above 2^27.
+// e4m3 rows become bf16 on the way, with their row's scale (exactly, but for
+// multiples of 2^-135 and 2^-134 at scale bytes 1 and 2: bf16's are 2^-133).  In the
+// probabilities the values' scales would take 1 % less time (64.2 us against 64.9,
+// batch 32, 8 KV heads of 128), but a small one leaves their terms below bf16's
+// range.
+// Queries and probabilities are taken as bf16 terms that hold all their bits:
+// bf16 queries are one, fp16 ones two, fp32 ones three, and so are probabilities,
+// whatever the output's type: of two terms a weight would be off by up to 2^-17 of
+// itself, and where values cancel a 16-bit output by many of its own half-steps
+// (two take 1 % less time: 49.7 us against 50.2 at batch 48, 32 KV heads of 64,
+// e4m3, fp16).  Softmax and sums are fp32; m moves only when a score is more than 8
+// / c above it, so the loop has no cross-lane step and no weight is above 1.  It is
+// taken from the scores before they are multiplied: c s - m would carry the
+// rounding of a product, more than 8 where scores are above 2^27.
 
 constexpr int kAttnWaves = 8;
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -123,18 +126,8 @@ __device__ __forceinline__ void join_parts(int n, float c, Joined &a, Get &&get)
     a.m = mn;
 }
 
-// Scale bytes of N consecutive positions, and the i-th.
-template <int N> struct ScaleWord;
-template <> struct ScaleWord<8> { typedef u32x2 type; };
-template <> struct ScaleWord<4> { typedef unsigned type; };
-template <> struct ScaleWord<2> { typedef uint16_t type; };
+// The i-th of 8 scale bytes.
 __device__ __forceinline__ unsigned scale_byte(u32x2 w, int i) { return (w[i / 4] >> (8 * (i & 3))) & 255u; }
-__device__ __forceinline__ unsigned scale_byte(unsigned w, int i) { return (w >> (8 * i)) & 255u; }
-
-// without the i-th
-__device__ __forceinline__ void clear_scale(u32x2 &w, int i) { w[i / 4] &= ~(255u << (8 * (i & 3))); }
-__device__ __forceinline__ void clear_scale(unsigned &w, int i) { w &= ~(255u << (8 * i)); }
-__device__ __forceinline__ void clear_scale(uint16_t &w, int i) { w &= (uint16_t)~(255u << (8 * i)); }
 
 // Two of a word's four e4m3 codes (the upper two: Hi) as bf16, times a power of two.
 template <bool Hi>
@@ -343,8 +336,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     };
     u32x4 kr[NS][2][NC];
     unsigned vr[NS][8][VW];
-    u32x2 ksr[NS];
-    typename ScaleWord<NV>::type vsr[NS];   // of the lane's NV positions
+    u32x2 ksr[NS], vsr[NS];
     typedef unsigned VWord __attribute__((ext_vector_type(VW)));
     bool page_bad = false;   // of the tile whose keys were asked for last
     // the first row of the group of positions at 'key', whose page lane 'from' of pages has
@@ -382,8 +374,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 #pragma unroll
                 for (int i = 0; i < VW; ++i) vr[s][j][i] = w[i];
             }
-            if constexpr (F8)
-                vsr[s] = *reinterpret_cast<const typename ScaleWord<NV>::type *>(p.c.vs + r0 + NV * copy);
+            if constexpr (F8) vsr[s] = *reinterpret_cast<const u32x2 *>(p.c.vs + r0);
         }
     };
 
@@ -517,23 +508,22 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         const int key0 = (a.t0 + a.t) * NK;
         const bool inside = key0 >= a.start && key0 + NK <= a.len;
         if (!inside) {
-            // what is masked may hold anything: its scores, values and scales go
+            // what is masked may hold anything: its scores, values and scales go (of a
+            // scale byte of 255 a zero code, too, would be NaN)
 #pragma unroll
             for (int sb = 0; sb < NS; ++sb) {
                 const int k0 = key0 + 32 * sb + 8 * k4;
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
                     const int key = k0 + NV * copy + v;
-                    if (key < a.start || key >= a.len) {
-                        s[sb][v] = -INFINITY;
-                        if constexpr (F8) clear_scale(vsr[sb], v);
-                    }
+                    if (key < a.start || key >= a.len) s[sb][v] = -INFINITY;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const bool out = k0 + j < a.start || k0 + j >= a.len;
 #pragma unroll
                     for (int i = 0; i < VW; ++i) vr[sb][j][i] = out ? 0u : vr[sb][j][i];
+                    if constexpr (F8) vsr[sb][j / 4] &= out ? ~(255u << (8 * (j & 3))) : ~0u;
                 }
             }
         }
@@ -557,7 +547,6 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             for (int v = 0; v < NV; ++v) {
                 pr[v] = __builtin_amdgcn_exp2f(fmaf(s[sb][v] - m, c, -8.f));
                 l += pr[v];
-                if constexpr (F8) pr[v] *= pow2_of(scale_byte(vsr[sb], v));
             }
             // this lane's column has the weights of its own positions and
             // zeros for the other copies'
@@ -587,12 +576,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
                 for (int j = 0; j < 4; ++j) {
                     const unsigned v0 = vr[sb][2 * j][w], v1 = vr[sb][2 * j + 1][w];
                     if constexpr (F8) {
-                        const unsigned u0 = __builtin_amdgcn_perm(v1, v0, 0x05010400);
-                        const unsigned u1 = __builtin_amdgcn_perm(v1, v0, 0x07030602);
-                        e[0][j] = fp8_to_bf16<false>(u0, 1.f);
-                        e[1][j] = fp8_to_bf16<true>(u0, 1.f);
-                        e[2][j] = fp8_to_bf16<false>(u1, 1.f);
-                        e[3][j] = fp8_to_bf16<true>(u1, 1.f);
+                        const float s0 = pow2_of(scale_byte(vsr[sb], 2 * j));
+                        const float s1 = pow2_of(scale_byte(vsr[sb], 2 * j + 1));
+                        const unsigned a0 = fp8_to_bf16<false>(v0, s0), a1 = fp8_to_bf16<true>(v0, s0);
+                        const unsigned b0 = fp8_to_bf16<false>(v1, s1), b1 = fp8_to_bf16<true>(v1, s1);
+                        e[0][j] = __builtin_amdgcn_perm(b0, a0, 0x05040100);
+                        e[1][j] = __builtin_amdgcn_perm(b0, a0, 0x07060302);
+                        e[2][j] = __builtin_amdgcn_perm(b1, a1, 0x05040100);
+                        e[3][j] = __builtin_amdgcn_perm(b1, a1, 0x07060302);
                     } else {
                         e[0][j] = __builtin_amdgcn_perm(v1, v0, 0x05040100);
                         e[1][j] = __builtin_amdgcn_perm(v1, v0, 0x07060302);

@@ -491,6 +491,44 @@ def test_attention_where_values_cancel(cache, io, d, group):
     check_attention(out, lse, (want[0], want[1], 2.0 ** -19.4 * mag, want[3]))
 
 
+@pytest.mark.parametrize("io", [BF16, FP32])
+@pytest.mark.parametrize("d,group", [(64, 1), (128, 4), (128, 16)])
+def test_attention_of_the_smallest_scales(io, d, group):
+    # An e4m3 pool's smallest scales, beside large ones or alone.  The weights are 2^-8
+    # times p or less, and nearly equal (scores differ by 0.05 at most): of n values three
+    # products each are rounded by 2^-150 at most, 3 2^-142 / 0.95 < 2^-140 of the output.
+    # Values are taken as bf16, whose smallest step is 2^-133: at scale bytes 1 and 2
+    # (random codes) off by 2^-134 at most, as a bf16 output of that size is.
+    n, page = 300, 16
+    pos = torch.arange(n, dtype=torch.int32).cuda()
+    for what in (448 * 2.0 ** -126, 1e-34, 1e-32, 1e-28, "apart", "codes"):
+        pool = make_pool(1, 20, 1, page, d, E4M3, gen(3))
+        k = torch.zeros(n, 1, d)
+        k[:, 0, 0] = torch.arange(n).float() * 0.125
+        v = torch.rand(n, 1, d, generator=gen(9)) * 0.5 + 0.5
+        if what == "apart":
+            v *= 1e-34
+            v[::2] = 0.0
+            v[:, :, 0] = 0.0
+            v[::2, :, 0] = 1e30
+        elif what != "codes":
+            v *= what
+        table = make_table([n], page, 20, gen(4))
+        pool.append(0, table.cuda(), pos, k.cuda(), v.cuda(), seq=torch.zeros_like(pos))
+        if what == "codes":
+            codes = torch.randint(0, 127, pool.v.shape, generator=gen(10), dtype=torch.uint8)
+            codes += 128 * torch.randint(0, 2, codes.shape, generator=gen(12), dtype=torch.uint8)
+            pool.v.view(torch.uint8).copy_(codes)
+            pool.v_scale.copy_(torch.randint(1, 4, pool.v_scale.shape, generator=gen(11), dtype=torch.uint8))
+        q = torch.zeros(1, group, d)
+        q[:, 0, 0] = 0.01
+        q = q.to(io)
+        o, l, tol, ltol = attention64(values(pool, "k"), values(pool, "v"), table, [n], q, page, d ** -0.5)
+        tol = tol + 2.0 ** -140 + (2.0 ** -133 if what == "codes" else 0.0)
+        out, lse = run_attention(pool, table, [n], q, page)
+        check_attention(out, lse, (o, l, tol, ltol), f"{what}")
+
+
 def garbage(pool, used):
     """Everything that no attended position uses: NaN, infinities, and scale bytes of all kinds."""
     for name in ("k", "v"):

@@ -288,8 +288,11 @@ class PagedKvCache:
                               workspace.numel(), self.error.data_ptr(), self._stream(stream))
 
     def device_error(self) -> int:
-        """Synchronizes; the error bits of this pool's calls so far, which are then cleared."""
+        """Waits for all of the device's streams; the error bits of this pool's calls so
+        far, which are then cleared (before any later call on any stream)."""
+        torch.cuda.synchronize(self.device)
         code = int(self.error.item())
         if code:
             self.error.zero_()
+            torch.cuda.synchronize(self.device)
         return code

@@ -807,6 +807,22 @@ def test_a_stream_of_the_caller():
     assert torch.equal(a, b)
 
 
+def test_device_error_sees_calls_of_other_streams():
+    pool = make_pool(1, 4, 2, 16, 64, BF16, gen(44))
+    table = torch.tensor([[0, 9]], dtype=torch.int32).cuda()   # (no page 9)
+    pos = torch.tensor([20], dtype=torch.int32).cuda()
+    row = torch.zeros(1, 2, 64, device="cuda")
+    side, work = torch.cuda.Stream(), torch.zeros(2048, 2048, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(40):
+                work @ work
+        pool.append(0, table, pos, row, row, stream=side)
+        assert pool.device_error() == kb.KL_DEVERR_PAGE
+        assert pool.device_error() == 0
+
+
 def test_the_contiguous_cache_and_pages():
     """A sequence goes from a contiguous cache into pages and back, bit for bit."""
     g = gen(43)

@@ -211,6 +211,13 @@ class PagedKvCache:
             k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
             None if v_scale is None else v_scale.data_ptr(), _DTYPES[k.dtype], L, pages, n_kv, ps, d,
             self.device.index)
+        self._filled()
+
+    def _filled(self) -> None:
+        """What has been filled on the current stream is there for calls on any stream
+        (in a capture the fill is a part of the graph instead, before the calls there)."""
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()
 
     def _table(self, table: torch.Tensor) -> kb.kl_page_table:
         (batch, n), (row, one) = table.shape, table.stride()
@@ -260,11 +267,13 @@ class PagedKvCache:
     def workspace(self, batch: int) -> torch.Tensor:
         """A workspace for attention calls of up to 'batch' sequences, one after
         the other (calls that may overlap, graphs replayed side by side
-        included, need one each)."""
+        included, need one each), on any stream."""
         n = kb.kl_paged_attention_workspace(self.c, batch)
         if n == 0:
             raise kb.KlError(kb.KL_ERR_INVALID_ARGUMENT, kb.kl_last_error())
-        return torch.zeros(n, dtype=torch.uint8, device=self.device)
+        ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        self._filled()
+        return ws
 
     def attention(self, layer: int, table: torch.Tensor, lengths: torch.Tensor, q: torch.Tensor,
                   out: torch.Tensor, workspace: torch.Tensor, scale: float | None = None,

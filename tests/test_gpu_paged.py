@@ -823,6 +823,46 @@ def test_device_error_sees_calls_of_other_streams():
         assert pool.device_error() == 0
 
 
+def test_a_pool_and_its_workspace_are_ready_for_any_stream():
+    # made while the current stream is busy, used at once on another
+    g = gen(45)
+    n, q = torch.tensor([900], dtype=torch.int32).cuda(), torch.randn(1, 16, 128, generator=g).cuda()
+    base = make_pool(1, 60, 2, 16, 128, E4M3, g)
+    table = make_table([900], 16, 60, g).cuda()
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    base.attention(0, table, n, q, want, base.workspace(1))
+    side, work = torch.cuda.Stream(), torch.zeros(2048, 2048, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out.fill_(5.0)
+        torch.cuda.synchronize()
+        for _ in range(40):
+            work @ work
+        pool = PagedKvCache.from_tensors(base.k, base.v, base.k_scale, base.v_scale)
+        pool.attention(0, table, n, q, out, pool.workspace(1), stream=side)
+        side.synchronize()
+        assert torch.equal(out, want)
+        assert pool.device_error() == 0
+
+
+def test_a_workspace_made_in_a_capture():
+    g = gen(46)
+    pool = make_pool(1, 60, 2, 16, 128, BF16, g)
+    table = make_table([900], 16, 60, g).cuda()
+    n, q = torch.tensor([900], dtype=torch.int32).cuda(), torch.randn(1, 16, 128, generator=g).cuda()
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    pool.attention(0, table, n, q, want, pool.workspace(1))
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        pool.attention(0, table, n, q, out, pool.workspace(1), stream=stream)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
 def test_the_contiguous_cache_and_pages():
     """A sequence goes from a contiguous cache into pages and back, bit for bit."""
     g = gen(43)

@@ -90,15 +90,22 @@ class GpuModel:
     def device_error(self) -> int:
         return kb.kl_get_device_error(self.state)
 
+    def _batch(self, tokens, positions, logits, hidden, device) -> int:
+        """The batch of a step's tensors, which are contiguous and on the cache's device."""
+        B = tokens.numel()
+        assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
+        assert positions.numel() == B
+        assert logits.dtype == torch.float32 and logits.shape == (B, self.model_cfg["vocab"])
+        if hidden is not None:
+            assert hidden.dtype == torch.float32 and hidden.shape == (B, self.model_cfg["hidden"])
+        for x in (tokens, positions, logits, hidden):
+            assert x is None or (x.is_contiguous() and x.device == device)
+        return B
+
     def step(self, tokens: torch.Tensor, positions: torch.Tensor, kv: "KvCache",
              logits: torch.Tensor, hidden: torch.Tensor | None, mode: int,
              stream: torch.cuda.Stream | None = None) -> None:
-        assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
-        assert logits.dtype == torch.float32 and logits.is_contiguous()
-        B = tokens.numel()
-        assert logits.shape == (B, self.model_cfg["vocab"])
-        if hidden is not None:
-            assert hidden.dtype == torch.float32 and hidden.shape == (B, self.model_cfg["hidden"])
+        B = self._batch(tokens, positions, logits, hidden, kv.k.device)
         kb.kl_decode_step(self.state, tokens.data_ptr(), positions.data_ptr(), B,
                           kv.k.data_ptr(), kv.v.data_ptr(), kv.batch, kv.capacity,
                           logits.data_ptr(), hidden.data_ptr() if hidden is not None else None,
@@ -109,12 +116,7 @@ class GpuModel:
                    stream: torch.cuda.Stream | None = None) -> None:
         """step() over a paged cache: row b of the table holds sequence b's pages.
         May be captured into a graph."""
-        assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
-        assert logits.dtype == torch.float32 and logits.is_contiguous()
-        B = tokens.numel()
-        assert logits.shape == (B, self.model_cfg["vocab"])
-        if hidden is not None:
-            assert hidden.dtype == torch.float32 and hidden.shape == (B, self.model_cfg["hidden"])
+        B = self._batch(tokens, positions, logits, hidden, pool.device)
         kb.kl_decode_step_paged(self.state, tokens.data_ptr(), positions.data_ptr(), B, pool.c,
                                 pool._table(table), logits.data_ptr(),
                                 hidden.data_ptr() if hidden is not None else None,
@@ -123,10 +125,9 @@ class GpuModel:
     def greedy(self, tokens: torch.Tensor, positions: torch.Tensor, kv: "KvCache", n_steps: int,
                tokens_out: torch.Tensor, logits: torch.Tensor, mode: int,
                stream: torch.cuda.Stream | None = None) -> None:
-        assert tokens.dtype == torch.int32 and positions.dtype == torch.int32
-        B = tokens.numel()
+        B = self._batch(tokens, positions, logits, None, kv.k.device)
         assert tokens_out.dtype == torch.int32 and tokens_out.shape == (n_steps, B)
-        assert logits.dtype == torch.float32 and logits.shape == (B, self.model_cfg["vocab"])
+        assert tokens_out.is_contiguous() and tokens_out.device == kv.k.device
         kb.kl_decode_greedy(self.state, tokens.data_ptr(), positions.data_ptr(), B, n_steps,
                             kv.k.data_ptr(), kv.v.data_ptr(), kv.batch, kv.capacity,
                             tokens_out.data_ptr(), logits.data_ptr(), stream_handle(stream), mode)

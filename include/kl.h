@@ -340,7 +340,7 @@ size_t kl_paged_attention_workspace(const kl_paged_cache *cache, int32_t batch);
  *   q, out     n_heads heads; n_heads a multiple of n_kv_heads, at most 16
  *              times as many
  *              (out overlaps neither q nor the pool)
- *   scale      finite
+ *   scale      at most 2^127 in magnitude (scores are taken times log2 e)
  *   lse        dev fp32 [batch][n_heads] or NULL: max_j + ln sum_j of scale q.k
  *              (what joins this result with one over other positions)
  *   workspace  dev, 16-byte aligned, at least kl_paged_attention_workspace()

@@ -207,7 +207,9 @@ kl_status kl_paged_attention(const kl_paged_cache *cache, int32_t layer,
     if (st != KL_OK) return st;
     st = check_rows(out, B, n_heads, c.head_dim, true, "out", who);
     if (st != KL_OK) return st;
-    if (!std::isfinite(scale)) return fail(KL_ERR_INVALID_ARGUMENT, "%s: scale is not finite", who);
+    // (times log2 e it has to be finite)
+    if (!(std::fabs(scale) <= 0x1p127f))
+        return fail(KL_ERR_INVALID_ARGUMENT, "%s: scale is not at most 2^127 in magnitude", who);
     if (window < 0) return fail(KL_ERR_INVALID_ARGUMENT, "%s: window %d < 0", who, window);
     if (!workspace || !aligned(workspace, 16) ||
         workspace_bytes < kl_paged_attention_workspace(cache, B))

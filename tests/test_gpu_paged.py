@@ -293,6 +293,29 @@ def test_attention_scales(cache, scale):
     check_attention(out, lse, want)
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("scale,query,key", [(2.0 ** 127, 2.0 ** -100, 2.0 ** -29),
+                                             (-2.0 ** 127, 2.0 ** -100, 2.0 ** -29),
+                                             (2.0 ** -126, 2.0 ** 62, 2.0 ** 60),
+                                             (2.0 ** -140, 2.0 ** 62, 2.0 ** 60)])
+def test_attention_of_the_largest_and_smallest_scales(cache, scale, query, key):
+    # keys are multiples of 'key' of 4 significant bits: scores in steps of 1/4 (or, of the
+    # smallest scale, next to none)
+    d, n, page = 64, 300, 16
+    pool = make_pool(1, 20, 1, page, d, cache, gen(3))
+    table = make_table([n], page, 20, gen(4))
+    k = torch.zeros(n, 1, d)
+    k[:, 0, 0] = torch.randint(-15, 16, (n,), generator=gen(8)).float() * key
+    pos = torch.arange(n, dtype=torch.int32).cuda()
+    pool.append(0, table.cuda(), pos, k.cuda(), torch.randn(n, 1, d, generator=gen(9)).cuda(),
+                seq=torch.zeros_like(pos))
+    q = torch.zeros(1, 3, d)
+    q[:, 0, 0], q[:, 1, 0] = query, -query
+    want = attention64(values(pool, "k"), values(pool, "v"), table, [n], q, page, scale)
+    out, lse = run_attention(pool, table, [n], q, page, scale=scale)
+    check_attention(out, lse, want)
+
+
 def test_attention_rising_and_falling_scores():
     # the running maximum rises at every position, or never after the first
     d, n, page = 128, 700, 16

@@ -114,6 +114,17 @@ def test_attention_refuses(over, status, msg):
     assert msg in kb.kl_last_error()
 
 
+@pytest.mark.parametrize("scale", [3.0e38, -3.0e38, 2.0 ** 127 * (1 + 2.0 ** -23)])
+def test_attention_refuses_scales_that_overflow(scale):
+    # log2(e) times such a scale may be infinite
+    assert call_attention(scale=scale) == kb.KL_ERR_INVALID_ARGUMENT
+    assert "2^127" in kb.kl_last_error()
+    # (no GPU here: the device check that follows the arguments' may fail)
+    assert call_attention(scale=2.0 ** 127, c=cache(device=77)) in (kb.KL_ERR_INVALID_ARGUMENT,
+                                                                    kb.KL_ERR_HIP)
+    assert "2^127" not in kb.kl_last_error()
+
+
 def test_workspace_bytes():
     L = kb.lib()
     n = L.kl_paged_attention_workspace(cache(), 1)

@@ -269,7 +269,8 @@ typedef enum {
  * v_scale: dev [n_layers][n_pages][n_kv_heads][page_size], 8-byte aligned
  * (NULL with KL_DTYPE_BF16).  A power of two costs an 8-bit float no
  * precision (the significand is scaled by nothing), every product with it is
- * exact, and a value read back is exact in bf16.
+ * exact in fp32, and from s = 3 on in bf16 (at 1 and 2 the smallest codes are
+ * multiples of 2^-135 and 2^-134, bf16's least step is 2^-133).
  * page_size: a power of two, 8..4096.  head_dim: 64 or 128.  device: the HIP
  * device of the pool, current in every call. */
 typedef struct {
@@ -282,7 +283,8 @@ typedef struct {
 
 /* Which pages hold a sequence: position p of sequence b is in page
  * pages[b * stride + p / page_size] at offset p % page_size (dev int32,
- * stride >= max_pages elements).  Only entries of positions in use are read.
+ * stride >= max_pages elements).  Entries of positions not in use may hold
+ * anything.
  * max_pages * page_size <= 2^30. */
 typedef struct {
     const int32_t *pages;

@@ -169,8 +169,8 @@ class PagedKvCache:
     [L][pages][n_kv][page_size][d], bf16 or e4m3; an e4m3 pool has a scale byte
     (biased exponent of a power of two) per row in k_scale and v_scale
     [L][pages][n_kv][page_size].  Which pages hold a sequence is the caller's
-    to decide: a table [batch][max_pages] int32 of page numbers, of which only
-    those of positions in use are read."""
+    to decide: a table [batch][max_pages] int32 of page numbers, of which those
+    of positions not in use may be anything."""
 
     def __init__(self, model_cfg: dict, n_pages: int, page_size: int = 64,
                  dtype: torch.dtype = torch.bfloat16, device="cuda"):

@@ -215,6 +215,31 @@ def test_read_gives_the_values_back(cache, io, d, kv, page):
     assert pool.device_error() == 0
 
 
+@pytest.mark.parametrize("io", [BF16, FP16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_read_of_the_smallest_scales_rounds_once(io, d):
+    # every code at scale bytes 1 to 4 (and the largest that append writes): exact in fp32,
+    # in bf16 rounded where codes are multiples of less than 2^-133
+    page, kv = 16, 2
+    for rows in (3, 2000):   # (few and many: different kernels)
+        n_pages = -(-rows // page)
+        pool = make_pool(1, n_pages, kv, page, d, E4M3, gen(2))
+        for name in ("k", "v"):
+            codes = torch.randint(0, 127, pool.k.shape, generator=gen(10), dtype=torch.uint8)
+            codes += 128 * torch.randint(0, 2, codes.shape, generator=gen(12), dtype=torch.uint8)
+            getattr(pool, name).view(torch.uint8).copy_(codes)
+            scale = torch.randint(1, 5, codes.shape[:-1], generator=gen(11), dtype=torch.uint8)
+            scale[..., 0] = 246   # (448 2^119 is a number of every type but fp16)
+            getattr(pool, name + "_scale").copy_(scale)
+        table = make_table([rows], page, n_pages, gen(4))
+        pos = torch.arange(rows, dtype=torch.int32)
+        out = [torch.full((rows, kv, d), 3.0, dtype=io, device="cuda") for _ in range(2)]
+        pool.read(0, table.cuda(), pos.cuda(), out[0], out[1], seq=torch.zeros_like(pos).cuda())
+        pg, off = table[0, pos.long() // page].long(), pos.long() % page
+        for o, name in zip(out, ("k", "v")):
+            assert torch.equal(o.cpu(), values(pool, name)[0][pg, :, off].to(io))
+
+
 # ---------------------------------------------------------------- attention
 
 def run_attention(pool, table, lengths, q, page, layer=0, scale=None, window=0, dtype=None, ws=None):

@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
     constexpr int NC = RB / 64;                 // 16-byte loads of a key row per lane
     constexpr int EV = D / 16, VW = EV * ES / 4;   // value elements, words per lane and position
     constexpr int ST = D / 32;                  // steps of the first product
-    constexpr int PT = 3;                       // terms of probabilities (QT: of queries)
-    constexpr bool kIsBf16 = QT == 1;           // the queries
+    constexpr int PT = 3;                       // terms of probabilities
+    constexpr bool kIsBf16 = QT == 1;           // queries: bf16, fp16, fp32 in 1, 2, 3 terms
     constexpr int NV = 8 / C;                   // scores of a block that a lane goes on with
     constexpr int WD = D + 2;                   // floats of a part of one head
     constexpr int NE = 2 * kAttnWaves;          // parts in LDS
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
 
     // The queries of a unit as columns of the first product: asked for as they
     // are, and taken apart into terms when they are needed.
-    constexpr int QW = QT < 3 ? 1 : 2;   // 16-byte words of 8 elements, at most
+    constexpr int QW = QT < 3 ? 1 : 2;   // 16-byte words of 8 elements
     bf16x8 q[QT][ST];
     auto ask_q = [&](const At &a, u32x4 (&raw)[ST][QW]) {
 #pragma unroll
@@ -388,13 +388,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
             const int d0 = F8 ? 64 * (s / 2) + 16 * k4 + 8 * (s & 1) : 32 * s + 8 * k4;
             // (columns past the group: head 0 again, masked below)
             const long long at = a.b * p.q_row + (a.g * G + (head < G ? head : 0)) * p.q_head + d0;
-            const float *f = reinterpret_cast<const float *>(p.q) + at;
-            if (QW == 2 && p.q_type == KL_DTYPE_FP32) {
+            if constexpr (QT == 3) {
+                const float *f = reinterpret_cast<const float *>(p.q) + at;
                 raw[s][0] = load_16B<false>(f, p.q_vec);
-                raw[s][QW - 1] = load_16B<false>(f + 4, p.q_vec);
+                raw[s][1] = load_16B<false>(f + 4, p.q_vec);
             } else {
                 raw[s][0] = load_16B<false>(reinterpret_cast<const uint16_t *>(p.q) + at, p.q_vec);
-                raw[s][QW - 1] = raw[s][0];
             }
         }
     };
@@ -404,7 +403,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         for (int s = 0; s < ST; ++s) {
             if constexpr (!kIsBf16) {
                 float v[8];
-                words_to_f32(raw[s][0], raw[s][QW - 1], p.q_type, v);
+                words_to_f32(raw[s][0], raw[s][QW - 1], QT == 3 ? KL_DTYPE_FP32 : KL_DTYPE_FP16, v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = head < G ? v[j] * sign : 0.f;
                 bf16x8 t[QT];
@@ -854,7 +853,7 @@ static hipError_t launch_attention(const AttnParams &p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// The instance for the pool's type, the terms and the group's copies.
+// The instance for the pool's type, the queries' terms and the group's copies.
 template <int D, bool F8, int QT>
 static hipError_t launch_copies(const AttnParams &p, hipStream_t stream) {
     if (p.group <= 4) return launch_attention<D, F8, QT, 4>(p, stream);
@@ -863,8 +862,7 @@ static hipError_t launch_copies(const AttnParams &p, hipStream_t stream) {
 }
 template <int D, bool F8>
 static hipError_t launch_terms(const AttnParams &p, hipStream_t stream) {
-    if (p.q_type == KL_DTYPE_FP32 || p.out_type == KL_DTYPE_FP32 || p.out_lo)
-        return launch_copies<D, F8, 3>(p, stream);
+    if (p.q_type == KL_DTYPE_FP32) return launch_copies<D, F8, 3>(p, stream);
     return p.q_type == KL_DTYPE_FP16 ? launch_copies<D, F8, 2>(p, stream)
                                      : launch_copies<D, F8, 1>(p, stream);
 }

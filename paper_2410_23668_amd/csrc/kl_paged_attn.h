@@ -15,8 +15,8 @@ namespace kl {
 // less.
 //
 // Split-K flash decoding over pages, bound by HBM: at 262144 positions of 8 KV
-// heads 6.1 TB/s bf16, 5.7 e4m3 and 5.0 at head dimension 64 (a read stream:
-// 6.8), and 6.45 TB/s for what is added to a long sequence; about 9 us stand
+// heads 6.1 TB/s bf16, 5.6 e4m3 and, e4m3 at head dimension 64, 5.0 (a read stream:
+// 6.8), and 6.4 TB/s for what is added to a long sequence; about 9 us stand
 // before the first tile (three round trips: lengths, pages, rows) and behind the
 // last (joins, two more).
 //
@@ -318,9 +318,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) kl_paged_attention_kernel(Att
         return a;
     };
 
-    // Loads, non-temporal: 94 us where ordinary ones take 105 (batch 16, 8192
-    // positions, 64 heads on 8 of 128, bf16), but for values of 64-byte rows: 52 us
-    // against 53.5 (batch 48, 32 KV heads of 64, e4m3).
+    // Loads, non-temporal: 94 us where ordinary ones take 104 (batch 16, 8192
+    // positions, 64 heads on 8 of 128, bf16), but for values of 64-byte rows: 51.8 us
+    // against 53.3 (batch 48, 32 KV heads of 64, e4m3).
     //
     // Every tile is asked for in the same way, without branches (behind a branch
     // around loads the compiler has to wait for all that may be in flight): a

@@ -54,10 +54,8 @@ struct Shares {
 //                        load and join, as long as a unit's parts are read in
 //                        one go (kHalfParts of them).
 // 32 heads on 8 of 128, bf16, one sequence, half rounds against whole: 1024
-// positions 10.7 us against 11.7, 2048 11.5 against 12.2; 4096, 32 parts, 14.8
-// against 13.6; shares of 2 tiles: 1024 11.1, 2048 12.7.  Against a unit of more
-// rounds in one workgroup: 512 positions 10.4 against 11.5 in two, 768 10.5 against
-// 11.6 in three (but 384, a round and a half, 10.4 against 10.3).
+// positions 10.9 us against 12.3, 2048 11.6 against 12.5; 4096, 32 parts, 14.7
+// against 13.6; shares of 2 tiles: 1024 11.2, 2048, 32 parts, 13.8.
 constexpr int kHalfShare = 4, kHalfParts = 16;
 KL_HD inline int equal_rounds(int T, int groups, int waves) {
     const int each = (T + groups - 1) / groups;
